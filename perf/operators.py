@@ -201,7 +201,7 @@ def prepare(case, seed):
         if "pos" in s:
             s["batch"] = qp.KVBatch(s["pos"], slots=s.get("slots"), start=s.get("start"), tokens=s["tokens"], max_new=case.get("new", 1))
         if case["op"] == "attend":
-            s["plan"] = s["ctx"].qp_kv_attention_plan(s["cache"], s["batch"], case["q_heads"], _DTYPES[case["dtype"]], window=case["window"])
+            s["plan"] = s["ctx"].qp_kv_attention_plan(s["cache"], case["q_heads"], window=case["window"])
     return s
 
 
