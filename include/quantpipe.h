@@ -67,6 +67,8 @@ enum { QP_B_MAD = 0 /* sum|x-mean|/N */, QP_B_MEAN_ABS = 1 /* sum|x|/N, the form
 #define QP_DEV_NONFINITE 4u
 #define QP_DEV_STREAM_TIMEOUT 8u  /* a bounded wait for a tile copy ran out; results of that call are invalid */
 #define QP_DEV_HIST_MISSING 16u   /* a search was promised a histogram in the statistics (QP_B_HIST_IN_STATS) that is not there */
+#define QP_DEV_KV_RANGE 64u       /* a slot, position or page outside the cache, or one listed twice where that is refused: skipped (see qp_kv_*) */
+#define QP_DEV_KV_EXHAUSTED 128u  /* too few free pages: the call changed nothing (see qp_kv_extend, qp_kv_fork) */
 #define QP_DEV_INDEX_RANGE 32u    /* debug build only: an index into a shared-memory or scratch table was out of range (redirected to entry 0) */
 
 /* Per-tensor statistics (Sec. 3: min/max of naive PTQ; mean and Laplace scale b of ACIQ;
@@ -560,6 +562,125 @@ int32_t qp_sender_host(qp_ctx* ctx, const void* h_x, int dtype, uint64_t n, int 
                        uint64_t packed_capacity, qp_qparams_t* h_qp_out, void* stream);
 int32_t qp_receiver_host(qp_ctx* ctx, const void* h_packed, uint64_t n, int bits, const qp_qparams_t* h_qp,
                          void* d_packed_work, void* d_y_work, void* h_y, int out_dtype, void* stream);
+
+/* ---- cache of keys and values in 4 bits (a variant of this library; the paper quantizes activations
+ * between stages, and has no cache) ----------------------------------------------------------------
+ * A stage that decodes keeps the keys and values of every token it has seen.  This cache keeps each of
+ * them as the token-wise variant sends a token: the row of head_dim elements of one (token, head) is
+ * quantized to 4 bits with a quantizer of its own under the min/max clip (QP_CLIP_MINMAX), so its codes
+ * are those of qp_stats_tokens + qp_clip_qparams_tokens_device + qp_quantize_pack_tokens.  Attention
+ * reads the codes and never writes the values they stand for.
+ *
+ * Memory (all of it the caller's).  d_pool: [layers, num_pages, heads, page_size / 16] slices of
+ * 16 * (head_dim + 16) bytes, layers layer_stride bytes apart, the rest contiguous.  A slice holds 16
+ * consecutive tokens of one head:
+ *     K codes       16 rows of head_dim / 2 bytes (element 2i in the low, 2i + 1 in the high four bits of byte i)
+ *     K quantizers  16 pairs of floats (lo, scale)
+ *     V codes, V quantizers   likewise
+ * Element d of a row is fma(code, scale, lo) in fp32.  A row's quantizer: lo = min over the finite elements, scale
+ * = (max - min) / 15 and inv_scale = 15 / (max - min) as qp_make_qparams; code = rint((clamp(x) - lo) *
+ * inv_scale), each operation rounded to fp32; NaN gives code 0, +-Inf the nearer end.  A constant row, a row
+ * without a finite element (lo = 0) and a row whose inv_scale passes fp32 (max - min below 5e-38) have
+ * scale 0 and codes 0.  Where max - lo passes fp32, positions are taken from halves: (x / 2 - lo / 2) * (2 inv_scale).
+ *   d_table  [max_seqs, max_pages] int32: the pages of a sequence in order, -1 behind them.  A row of the
+ *            table is called a slot
+ *   d_lens   [max_seqs] int32: tokens of each slot (0: the slot is empty)
+ *   d_refs   [num_pages] int32: how many slots hold the page (0: it is free)
+ *   d_work   qp_kv_work_ints(cache) int32 of scratch for the page calls
+ * One block table serves all layers: page p of every layer belongs to the same tokens.  A fresh cache has
+ * table -1, lens 0 and refs 0.  One cache is used from one stream at a time.
+ *
+ * head_dim 64, 128 or 256; page_size a multiple of 16 up to 1024; d_pool and layer_stride multiples of 16
+ * (layer_stride is not looked at where layers is 1). */
+typedef struct {
+    void* d_pool;
+    uint64_t layer_stride;
+    int32_t *d_table, *d_lens, *d_refs, *d_work;
+    int32_t layers, num_pages, heads, head_dim, page_size, max_seqs, max_pages, reserved;
+} qp_kv_cache_t;             /* 80 bytes */
+
+/* The new tokens of a step.  Sequence b of the batch is slot d_slots[b] (NULL: slot b); its tokens are the rows
+ * d_start[b] .. d_start[b + 1] - 1 (NULL: row b alone) of the step's K, V and Q buffers, and the first of them has position
+ * d_pos[b] in the sequence.  d_pos[b] < 0: the sequence takes no part.  tokens bounds the rows of the
+ * buffers: rows behind d_start[batch] (or at and behind `tokens`) are neither read nor written.  max_new bounds the
+ * tokens of one sequence; what a sequence has beyond them is skipped with QP_DEV_KV_RANGE by qp_kv_extend
+ * (the whole sequence) and qp_kv_attention (the rows behind).  d_start ascends. */
+typedef struct {
+    const int32_t *d_slots, *d_start;
+    int32_t* d_pos;
+    int32_t batch, tokens, max_new, reserved;
+} qp_kv_batch_t;             /* 40 bytes */
+
+/* bytes of one slice (16 tokens of a head), 0 for a head_dim that is not supported; ints of d_work, 0 for sizes that are not */
+uint64_t qp_kv_slice_bytes(int head_dim);
+uint64_t qp_kv_work_ints(int32_t num_pages, int32_t max_seqs);
+
+/* Makes room: gives every sequence of the batch the pages that its new tokens need, writes d_pos[b] = d_lens[slot]
+ * and adds the new tokens to d_lens.  Pages are the free ones of lowest number, handed out in the batch's order
+ * and, within a sequence, in the table's.  If the free pages do not suffice for the whole batch, nothing changes, every
+ * d_pos[b] becomes -1 and QP_DEV_KV_EXHAUSTED is raised.  A sequence whose slot is out of range, was listed before in this
+ * batch, or would outgrow max_pages gets d_pos[b] = -1, QP_DEV_KV_RANGE is raised, and the others go on.
+ * batch <= max_seqs.  One launch.
+ * Errors of all qp_kv_* calls: QP_ERR_INVALID_ARG (null pointers, sizes), QP_ERR_ALIGNMENT, QP_ERR_UNSUPPORTED_DTYPE,
+ * QP_ERR_BUFFER_TOO_SMALL (workspace), QP_ERR_CUDA. */
+int32_t qp_kv_extend(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batch_t* h_batch, void* stream);
+
+/* Quantizes the step's keys and values into the pages.  d_k, d_v: row `token`, head h at element token * token_stride + h *
+ * head_stride (strides in elements), head_dim contiguous elements.  A token whose page the table does not name is skipped
+ * with QP_DEV_KV_RANGE.  Neither d_lens nor d_pos changes, so a second call writes the same rows again.  A sequence
+ * listed twice with the same positions leaves either's rows. */
+int32_t qp_kv_append(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batch_t* h_batch, int layer, const void* d_k,
+                     const void* d_v, int dtype, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                     int64_t v_head_stride, void* stream);
+
+/* The inverse: the batch's rows of the cache as the values that they stand for, in fp32 or bf16.  Rows of tokens that
+ * the cache does not hold are left as they were, with QP_DEV_KV_RANGE.  d_k or d_v may be NULL. */
+int32_t qp_kv_gather(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batch_t* h_batch, int layer, void* d_k, void* d_v,
+                     int dtype, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride, int64_t v_head_stride,
+                     void* stream);
+
+/* Attention of the batch's queries over the cache.  The token at position t of its sequence sees the keys u <= t and, with
+ * window > 0, u > t - window:
+ *     out = sum_u p_u v_u,  p = softmax_u(scale * q . k_u)
+ * with k_u and v_u the values that the cache's rows stand for.  q_heads is a multiple of the cache's heads; query head
+ * g reads the cached head g / (q_heads / heads).  The step's own tokens are in the cache before (qp_kv_append).  Scores, softmax
+ * and sums are fp32; out has q's type.  d_lse (or NULL): [tokens, q_heads] fp32, the natural logarithm of the sum
+ * of the exponentials.  A row that sees no key is 0 with lse -inf; a query with a non-finite element gives NaN in its row
+ * only.  A token on a page that the table does not name counts as masked, with QP_DEV_KV_RANGE.
+ * The plan holds what stays from call to call; its workspace belongs to one stream at a time and is zeroed once,
+ * before its first use (each call leaves its counters at zero). */
+typedef struct {
+    void* d_work;
+    uint64_t work_bytes;     /* at least qp_kv_attention_work_bytes */
+    int32_t q_heads, window; /* window 0: none */
+    float scale;
+    int32_t reserved;
+} qp_kv_attention_t;         /* 32 bytes */
+uint64_t qp_kv_attention_work_bytes(qp_ctx* ctx, const qp_kv_cache_t* h_cache);
+int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batch_t* h_batch, const qp_kv_attention_t* h_plan,
+                        int layer, const void* d_q, int dtype, int64_t q_token_stride, int64_t q_head_stride, void* d_out,
+                        int64_t out_token_stride, int64_t out_head_stride, float* d_lse, void* stream);
+
+/* Slot d_dst[i] becomes a copy of slot d_src[i], for n pairs at once, as the slots were before the call: full pages are
+ * shared (d_refs + 1), a part-filled last page is copied to a free page (lowest numbers first, in the pairs'
+ * order), so that no two sequences ever write to one page.  d_dst[i] has to be empty.  A pair with a slot out of range, a
+ * d_dst[i] that is not empty or was listed before, is skipped with QP_DEV_KV_RANGE.  Too few free pages: nothing changes,
+ * QP_DEV_KV_EXHAUSTED.  n <= max_seqs.  Two launches. */
+int32_t qp_kv_fork(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const int32_t* d_src, const int32_t* d_dst, int32_t n, void* stream);
+
+/* Empties n slots: d_refs of their pages - 1, table -1, length 0.  An empty slot, also one listed before, is left alone; a slot
+ * out of range is skipped with QP_DEV_KV_RANGE. */
+int32_t qp_kv_free(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const int32_t* d_slots, int32_t n, void* stream);
+
+/* Copies page d_src[i] to page d_dst[i] in every layer, n pairs at once; table and refs stay.  Skipped with QP_DEV_KV_RANGE: a
+ * pair with a page out of range, one whose d_dst was listed before, and one whose d_src is another pair's d_dst.
+ * n <= num_pages.  Two launches. */
+int32_t qp_kv_copy_pages(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const int32_t* d_src, const int32_t* d_dst, int32_t n,
+                         void* stream);
+
+/* Makes the pool dense: with L pages in use, the k-th free page below L takes the contents of the k-th used page at or above L,
+ * and table and refs follow; pages L .. num_pages - 1 are free afterwards.  d_live (or NULL): L.  Two launches. */
+int32_t qp_kv_compact(qp_ctx* ctx, const qp_kv_cache_t* h_cache, int32_t* d_live, void* stream);
 
 #ifdef __cplusplus
 }

@@ -29,6 +29,7 @@ QP_DIST_LAPLACE, QP_DIST_GAUSS = 0, 1
 QP_B_MAD, QP_B_MEAN_ABS = 0, 1
 QP_DEV_BITS_MISMATCH, QP_DEV_DEGENERATE, QP_DEV_NONFINITE, QP_DEV_STREAM_TIMEOUT, QP_DEV_HIST_MISSING = 1, 2, 4, 8, 16
 QP_DEV_INDEX_RANGE = 32
+QP_DEV_KV_RANGE, QP_DEV_KV_EXHAUSTED = 64, 128
 QP_DEFAULT_STEPS, QP_DEFAULT_HIST_BINS = 100, 100
 QP_SEARCH_AUTO, QP_SEARCH_CANDIDATES, QP_SEARCH_INTERVALS, QP_SEARCH_INTERVALS_PLAIN = 0, 1, 2, 3
 QP_SENDER_AUTO, QP_SENDER_CHAIN, QP_SENDER_FUSED = 0, 1, 2
@@ -49,6 +50,8 @@ EXPORTS = (
     "qp_stats_tokens", "qp_clip_qparams_tokens_device", "qp_quantize_pack_tokens", "qp_unpack_dequantize_tokens",
     "qp_sender_tokens_device",
     "qp_built_with_index_checks", "qp_set_stats_path", "qp_dsaciq_candidates", "qp_dsaciq_candidates_channels", "qp_set_wait_limit_for_testing",
+    "qp_kv_slice_bytes", "qp_kv_work_ints", "qp_kv_extend", "qp_kv_append", "qp_kv_gather", "qp_kv_attention_work_bytes",
+    "qp_kv_attention", "qp_kv_fork", "qp_kv_free", "qp_kv_copy_pages", "qp_kv_compact",
 )
 
 
@@ -75,6 +78,23 @@ class Controller(C.Structure):
                 ("overhead_bytes", C.c_uint64), ("rel_change", C.c_double), ("sum_bytes", C.c_double),
                 ("sum_seconds", C.c_double), ("ref_bandwidth_bps", C.c_double), ("n_allowed", C.c_int32),
                 ("allowed", C.c_int32 * 8)]
+
+
+class KVCacheDesc(C.Structure):
+    _fields_ = [("d_pool", C.c_void_p), ("layer_stride", C.c_uint64), ("d_table", C.c_void_p), ("d_lens", C.c_void_p),
+                ("d_refs", C.c_void_p), ("d_work", C.c_void_p), ("layers", C.c_int32), ("num_pages", C.c_int32),
+                ("heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32), ("max_seqs", C.c_int32),
+                ("max_pages", C.c_int32), ("reserved", C.c_int32)]
+
+
+class KVBatchDesc(C.Structure):
+    _fields_ = [("d_slots", C.c_void_p), ("d_start", C.c_void_p), ("d_pos", C.c_void_p), ("batch", C.c_int32),
+                ("tokens", C.c_int32), ("max_new", C.c_int32), ("reserved", C.c_int32)]
+
+
+class KVAttentionDesc(C.Structure):
+    _fields_ = [("d_work", C.c_void_p), ("work_bytes", C.c_uint64), ("q_heads", C.c_int32), ("window", C.c_int32),
+                ("scale", C.c_float), ("reserved", C.c_int32)]
 
 
 QP_CTRL_FIT, QP_CTRL_EQ2 = 0, 1
@@ -164,10 +184,26 @@ def load() -> C.CDLL:
                                  C.POINTER(QParams), vp]
     L.qp_sender_device.argtypes = [vp, vp, C.c_int, u64, C.c_int, C.c_int, C.c_int, C.c_int, C.c_int, vp, u64, vp, vp, vp]
     L.qp_receiver_host.argtypes = [vp, vp, u64, C.c_int, C.POINTER(QParams), vp, vp, vp, C.c_int, vp]
+    cache, batch, plan, i64 = C.POINTER(KVCacheDesc), C.POINTER(KVBatchDesc), C.POINTER(KVAttentionDesc), C.c_int64
+    L.qp_kv_slice_bytes.argtypes = [C.c_int]
+    L.qp_kv_slice_bytes.restype = u64
+    L.qp_kv_work_ints.argtypes = [i32, i32]
+    L.qp_kv_work_ints.restype = u64
+    L.qp_kv_attention_work_bytes.argtypes = [vp, cache]
+    L.qp_kv_attention_work_bytes.restype = u64
+    L.qp_kv_extend.argtypes = [vp, cache, batch, vp]
+    L.qp_kv_append.argtypes = [vp, cache, batch, C.c_int, vp, vp, C.c_int, i64, i64, i64, i64, vp]
+    L.qp_kv_gather.argtypes = [vp, cache, batch, C.c_int, vp, vp, C.c_int, i64, i64, i64, i64, vp]
+    L.qp_kv_attention.argtypes = [vp, cache, batch, plan, C.c_int, vp, C.c_int, i64, i64, vp, i64, i64, vp, vp]
+    L.qp_kv_fork.argtypes = [vp, cache, vp, vp, i32, vp]
+    L.qp_kv_free.argtypes = [vp, cache, vp, i32, vp]
+    L.qp_kv_copy_pages.argtypes = [vp, cache, vp, vp, i32, vp]
+    L.qp_kv_compact.argtypes = [vp, cache, vp, vp]
     for name in EXPORTS:
         fn = getattr(L, name)
         if name not in ("qp_last_error", "qp_status_string", "qp_packed_bytes", "qp_aciq_F", "qp_launch_count",
-                        "qp_controller_payload_bytes", "qp_graph_replays"):
+                        "qp_controller_payload_bytes", "qp_graph_replays", "qp_kv_slice_bytes", "qp_kv_work_ints",
+                        "qp_kv_attention_work_bytes"):
             fn.restype = i32
     _load_call_path(L)
     _lib = L
@@ -329,6 +365,93 @@ def _as_struct(t: torch.Tensor, cls):
     """Copies a device byte buffer holding one struct to the host (synchronises)."""
     raw = t.detach().cpu().contiguous().numpy().tobytes()
     return cls.from_buffer_copy(raw[:C.sizeof(cls)])
+
+
+# ------------------------------------------------------------ cache of keys and values in 4 bits
+
+def qp_kv_slice_bytes(head_dim: int) -> int:
+    """Bytes of 16 tokens of one head; 0 for a head_dim that is not supported."""
+    return int(load().qp_kv_slice_bytes(head_dim))
+
+
+def _ints(t: torch.Tensor, what: str, device, n: int | None = None) -> torch.Tensor:
+    if not (isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()):
+        raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} must be a contiguous int32 CUDA tensor")
+    if device is not None and t.device != device:
+        raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} is on another device")
+    if n is not None and t.numel() != n:
+        raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} must have {n} entries")
+    return t
+
+
+class KVCache:
+    """Keys and values of many sequences in 4 bits, in pages that one block table names for all layers.
+
+    pool [layers, pages, heads, page_size / 16, qp_kv_slice_bytes(head_dim)] uint8, each layer contiguous; table [slots, pages of a
+    sequence], lens [slots], refs [pages] int32.  KVCache.empty() makes a fresh one."""
+
+    def __init__(self, pool: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, refs: torch.Tensor, head_dim: int):
+        slice_bytes = qp_kv_slice_bytes(head_dim)
+        if not slice_bytes:
+            raise QuantPipeError(QP_ERR_INVALID_ARG, f"head_dim {head_dim} is not supported")
+        if not (pool.is_cuda and pool.dtype == torch.uint8 and pool.dim() == 5 and pool.shape[4] == slice_bytes and pool.shape[0] > 0
+                and pool[0].is_contiguous()):
+            raise QuantPipeError(QP_ERR_INVALID_ARG, "pool must be a CUDA tensor [layers, pages, heads, page_size / 16, "
+                                                     f"{slice_bytes}] of bytes, each layer contiguous")
+        layers, pages, heads, slices, _ = pool.shape
+        _ints(table, "table", pool.device), _ints(lens, "lens", pool.device), _ints(refs, "refs", pool.device, pages)
+        if table.dim() != 2 or lens.numel() != table.shape[0]:
+            raise QuantPipeError(QP_ERR_INVALID_ARG, "table must be [slots, pages of a sequence] and lens [slots]")
+        self.pool, self.table, self.lens, self.refs, self.head_dim = pool, table, lens, refs, head_dim
+        self.device, self.layers, self.pages, self.heads, self.page_size = pool.device, layers, pages, heads, 16 * slices
+        self.slots, self.max_pages = table.shape
+        work = int(load().qp_kv_work_ints(pages, self.slots))
+        self.work = torch.empty(max(work, 1), dtype=torch.int32, device=pool.device)
+        self._desc = KVCacheDesc(pool.data_ptr(), pool.stride(0) if layers > 1 else 0, table.data_ptr(), lens.data_ptr(),
+                                 refs.data_ptr(), self.work.data_ptr(), layers, pages, heads, head_dim, self.page_size, self.slots,
+                                 self.max_pages, 0)
+        self._at = C.addressof(self._desc)
+
+    @classmethod
+    def empty(cls, pages: int, heads: int, head_dim: int, slots: int, max_pages: int, page_size: int = 64, layers: int = 1,
+              device: int | torch.device = 0) -> "KVCache":
+        dev = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
+        slice_bytes = qp_kv_slice_bytes(head_dim)
+        if not slice_bytes or page_size < 16 or page_size % 16 or min(pages, heads, slots, max_pages, layers) < 1:
+            raise QuantPipeError(QP_ERR_INVALID_ARG, "sizes of the cache")
+        return cls(torch.empty(layers, pages, heads, page_size // 16, slice_bytes, dtype=torch.uint8, device=dev),
+                   torch.full((slots, max_pages), -1, dtype=torch.int32, device=dev),
+                   torch.zeros(slots, dtype=torch.int32, device=dev), torch.zeros(pages, dtype=torch.int32, device=dev), head_dim)
+
+
+class KVBatch:
+    """The new tokens of a step: pos [batch] (the position of each sequence's first), slots [batch] or None (slot b), start
+    [batch + 1] or None (one token each, row b).  tokens: rows of the step's tensors; max_new: most tokens of one sequence."""
+
+    def __init__(self, pos: torch.Tensor, slots: torch.Tensor | None = None, start: torch.Tensor | None = None,
+                 tokens: int | None = None, max_new: int | None = None):
+        _ints(pos, "pos", None)
+        n = pos.numel()
+        if slots is not None:
+            _ints(slots, "slots", pos.device, n)
+        if start is not None:
+            _ints(start, "start", pos.device, n + 1)
+            if tokens is None or max_new is None:
+                raise QuantPipeError(QP_ERR_INVALID_ARG, "tokens and max_new are needed with start")
+        self.pos, self.slots, self.start = pos, slots, start
+        self.batch, self.tokens, self.max_new = n, n if tokens is None else tokens, 1 if max_new is None else max_new
+        self._desc = KVBatchDesc(None if slots is None else slots.data_ptr(), None if start is None else start.data_ptr(),
+                                 pos.data_ptr(), self.batch, self.tokens, self.max_new, 0)
+        self._at = C.addressof(self._desc)
+
+
+class KVAttention:
+    """What attention over a cache keeps from call to call: its workspace (of one stream at a time) and its constants."""
+
+    def __init__(self, work: torch.Tensor, q_heads: int, window: int, scale: float):
+        self.work, self.q_heads, self.window, self.scale = work, q_heads, window, scale
+        self._desc = KVAttentionDesc(work.data_ptr(), work.nbytes, q_heads, window, scale, 0)
+        self._at = C.addressof(self._desc)
 
 
 class Context:
@@ -594,6 +717,95 @@ class Context:
         self._run("qp_sender_tokens_device", x, code, tokens, channels, bits, method, bmode, out_packed, out_packed.nbytes,
                   out_qp, stats_work)
         return out_packed, out_qp
+
+    # -- cache of keys and values in 4 bits
+    def _kv_rows(self, x: torch.Tensor, cache: KVCache, batch: KVBatch, heads: int, what: str) -> tuple:
+        """(token stride, head stride) of a [tokens, heads, head_dim] tensor of this device."""
+        if not (x.device == self.device and x.dim() == 3 and x.shape[0] >= batch.tokens and x.shape[1] == heads
+                and x.shape[2] == cache.head_dim and x.stride(2) == 1):
+            raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} must be [tokens, {heads}, {cache.head_dim}] on {self.device}, the last "
+                                                     f"dimension contiguous, tokens at least {batch.tokens}")
+        return x.stride(0), x.stride(1)
+
+    def _kv_here(self, *parts) -> None:
+        for p in parts:
+            t = p.pool if isinstance(p, KVCache) else p.pos if isinstance(p, KVBatch) else p
+            if t.device != self.device:
+                raise QuantPipeError(QP_ERR_INVALID_ARG, f"a cache, batch or list on {t.device}, the context on {self.device}")
+
+    def qp_kv_extend(self, cache: KVCache, batch: KVBatch) -> torch.Tensor:
+        """Pages for the batch's new tokens; fills and returns batch.pos and adds to cache.lens."""
+        self._kv_here(cache, batch)
+        self._run("qp_kv_extend", cache._at, batch._at)
+        return batch.pos
+
+    def qp_kv_append(self, cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, layer: int = 0) -> None:
+        """Quantizes the step's keys and values [tokens, heads, head_dim] into the cache's pages."""
+        self._kv_here(cache, batch)
+        kt, kh = self._kv_rows(k, cache, batch, cache.heads, "k")
+        vt, vh = self._kv_rows(v, cache, batch, cache.heads, "v")
+        if k.dtype != v.dtype:
+            raise QuantPipeError(QP_ERR_INVALID_ARG, "k and v of different types")
+        self._run("qp_kv_append", cache._at, batch._at, layer, k, v, _dtype_code(k), kt, kh, vt, vh)
+
+    def qp_kv_gather(self, cache: KVCache, batch: KVBatch, k: torch.Tensor | None = None, v: torch.Tensor | None = None,
+                     layer: int = 0, out_dtype: torch.dtype = torch.float32):
+        """The batch's rows of the cache as the values they stand for: into k and v, or (both None) two new tensors of zeros."""
+        self._kv_here(cache, batch)
+        if k is None and v is None:
+            k, v = torch.zeros(2, batch.tokens, cache.heads, cache.head_dim, dtype=out_dtype, device=self.device)
+        kt, kh = (0, 0) if k is None else self._kv_rows(k, cache, batch, cache.heads, "k")
+        vt, vh = (0, 0) if v is None else self._kv_rows(v, cache, batch, cache.heads, "v")
+        if k is not None and v is not None and k.dtype != v.dtype:
+            raise QuantPipeError(QP_ERR_INVALID_ARG, "k and v of different types")
+        self._run("qp_kv_gather", cache._at, batch._at, layer, k, v, _dtype_code(v if k is None else k), kt, kh, vt, vh)
+        return k, v
+
+    def qp_kv_attention_plan(self, cache: KVCache, q_heads: int, window: int = 0, scale: float | None = None) -> KVAttention:
+        """Workspace and constants of attention calls on this cache; scale None: head_dim ** -0.5."""
+        self._kv_here(cache)
+        work = torch.zeros(_call64(_addr["qp_kv_attention_work_bytes"], self._hv, cache._at), dtype=torch.uint8, device=self.device)
+        return KVAttention(work, q_heads, window, cache.head_dim ** -0.5 if scale is None else scale)
+
+    def qp_kv_attention(self, cache: KVCache, batch: KVBatch, q: torch.Tensor, plan: KVAttention, layer: int = 0,
+                        out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
+        """Attention of q [tokens, q_heads, head_dim] over the cache; writes out (q's type) and, if given, lse [tokens, q_heads]."""
+        self._kv_here(cache, batch, plan.work)
+        qt, qh = self._kv_rows(q, cache, batch, plan.q_heads, "q")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        ot, oh = self._kv_rows(out, cache, batch, plan.q_heads, "out")
+        if out.dtype != q.dtype:
+            raise QuantPipeError(QP_ERR_INVALID_ARG, "out must have q's type")
+        if lse is not None and not (lse.dtype == torch.float32 and lse.device == self.device and lse.is_contiguous()
+                                    and lse.numel() >= batch.tokens * plan.q_heads):
+            raise QuantPipeError(QP_ERR_INVALID_ARG, "lse must be a contiguous float32 tensor [tokens, q_heads]")
+        self._run("qp_kv_attention", cache._at, batch._at, plan._at, layer, q, _dtype_code(q), qt, qh, out, ot, oh, lse)
+        return out
+
+    def qp_kv_fork(self, cache: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:
+        """Slots dst become copies of slots src: full pages shared, a part-filled one copied."""
+        self._kv_here(cache)
+        _ints(src, "src", self.device), _ints(dst, "dst", self.device, src.numel())
+        self._run("qp_kv_fork", cache._at, src, dst, src.numel())
+
+    def qp_kv_free(self, cache: KVCache, slots: torch.Tensor) -> None:
+        self._kv_here(cache)
+        _ints(slots, "slots", self.device)
+        self._run("qp_kv_free", cache._at, slots, slots.numel())
+
+    def qp_kv_copy_pages(self, cache: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:
+        """Page dst[i] of every layer takes the bytes of page src[i]."""
+        self._kv_here(cache)
+        _ints(src, "src", self.device), _ints(dst, "dst", self.device, src.numel())
+        self._run("qp_kv_copy_pages", cache._at, src, dst, src.numel())
+
+    def qp_kv_compact(self, cache: KVCache, live: torch.Tensor | None = None) -> None:
+        """Moves the pages in use to the lowest numbers; live (one int32, or None) takes how many there are."""
+        self._kv_here(cache)
+        if live is not None:
+            _ints(live, "live", self.device, 1)
+        self._run("qp_kv_compact", cache._at, live)
 
     # -- host-buffer sender / receiver
     def qp_sender_host(self, h_x: torch.Tensor, bits: int, use_ds: bool, d_x_work: torch.Tensor,

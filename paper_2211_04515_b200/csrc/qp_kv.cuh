@@ -1,0 +1,71 @@
+// The 4-bit cache of keys and values, as its kernels see it: memory format, batch look-ups, argument checks.
+#pragma once
+
+#include "qp_internal.cuh"
+
+constexpr int QP_KV_SLICE = 16;                  // tokens of a slice
+constexpr int QP_KV_MAX_PAGE = 1024;
+
+static inline bool qp_kv_dim_ok(int d) { return d == 64 || d == 128 || d == 256; }
+
+// places inside a slice of 16 tokens
+template <int D>
+struct qp_kv_slice {
+    static constexpr int ROW = D / 2;                            // bytes of a row's codes
+    static constexpr int CODES = QP_KV_SLICE * ROW;
+    static constexpr int QUANT = QP_KV_SLICE * 8;
+    static constexpr int KQ = CODES, V = CODES + QUANT, VQ = 2 * CODES + QUANT;
+    static constexpr int BYTES = 2 * (CODES + QUANT);
+};
+
+int32_t qp_kv_check_cache(qp_ctx* ctx, const qp_kv_cache_t* c);                     // (qp_kv_rows.cu)
+int32_t qp_kv_check_batch(qp_ctx* ctx, const qp_kv_batch_t* b);
+int32_t qp_kv_check_layer(qp_ctx* ctx, const qp_kv_cache_t* c, int layer);
+
+#ifdef __CUDACC__
+
+// the batch, from the device's side
+struct qp_kv_rows {
+    const int32_t *slots, *start, *pos;
+    int batch, tokens;
+};
+static inline qp_kv_rows qp_kv_rows_of(const qp_kv_batch_t* b) { return {b->d_slots, b->d_start, b->d_pos, b->batch, b->tokens}; }
+
+__device__ __forceinline__ int qp_kv_start(const qp_kv_rows& r, int b)
+{
+    const int s = r.start ? __ldg(r.start + b) : b;
+    return s < 0 ? 0 : s > r.tokens ? r.tokens : s;
+}
+__device__ __forceinline__ int qp_kv_slot(const qp_kv_rows& r, int b) { return r.slots ? __ldg(r.slots + b) : b; }
+
+// sequence that row `token` belongs to, -1 if none: the last b with start[b] <= token, if token < start[b + 1]
+__device__ __forceinline__ int qp_kv_find(const qp_kv_rows& r, int token)
+{
+    if (!r.start) return token < r.batch ? token : -1;
+    int lo = 0, hi = r.batch;                                    // start[lo] <= token (or lo = 0), start[hi] > token
+    if (qp_kv_start(r, 0) > token || qp_kv_start(r, r.batch) <= token) return -1;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (qp_kv_start(r, mid) <= token) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+
+// page of token position p of a slot, -1 if the cache has none
+struct qp_kv_pages {
+    const int32_t* table;
+    int num_pages, page_size, max_seqs, max_pages;
+};
+static inline qp_kv_pages qp_kv_pages_of(const qp_kv_cache_t* c)
+{
+    return {c->d_table, c->num_pages, c->page_size, c->max_seqs, c->max_pages};
+}
+__device__ __forceinline__ int qp_kv_page(const qp_kv_pages& c, int slot, int p)
+{
+    const int i = p / c.page_size;
+    if (slot < 0 || slot >= c.max_seqs || p < 0 || i >= c.max_pages) return -1;
+    const int page = __ldg(c.table + (size_t)slot * c.max_pages + i);
+    return page >= 0 && page < c.num_pages ? page : -1;
+}
+
+#endif

@@ -1,0 +1,27 @@
+// What the attention kernels over the 4-bit cache are given.
+#pragma once
+
+#include <type_traits>
+
+#include "qp_kv.cuh"
+
+constexpr int QP_KV_MAX_DEVICES = 64;
+constexpr int QP_KV_COUNTERS = 4096;             // of a plan's workspace: one for each block
+
+struct qp_kv_attn_args {
+    qp_kv_rows rows;
+    qp_kv_pages pages;
+    const char* pool;                            // of the layer
+    int heads, slices;                           // cached heads, slices of a page
+    int q_heads, group, max_new, window;
+    float scale_log2;                            // scale * log2(e)
+    const void* q;
+    int64_t qt, qh;
+    void* out;
+    int64_t ot, oh;
+    float* lse;
+    bool vec;                                    // 16-byte loads of q
+    unsigned* count;
+    float* part;
+    unsigned* status;
+};
