@@ -17,9 +17,11 @@
 //     copies (a slice is contiguous), no barrier with other warps until its part of the sequence ends.
 //   - Softmax with a reference instead of the running maximum: p = 2^(s - m) where m is only raised, by a vote, once a score
 //     passes it by 8; the same for the scale of V, so that p * scale' fits fp16.
-//   - The work of the whole batch, in units of 64 tokens of one (sequence, head, tile of queries), is cut into equal runs, one
-//     for each resident block, whatever the lengths.  Where a cut falls inside an item, its blocks leave partial results,
-//     and the last to finish (a counter per item; nobody waits) adds them up in the blocks' order, so the result does not depend on timing.
+//   - The work of the whole batch, in units of 64 tokens of one item (sequence, head, tile of queries), is cut into equal runs, one
+//     for each resident block, whatever the lengths; an item counts HEAD units more than it has, for what its beginning and end
+//     cost.  Where a cut falls inside an item, its blocks leave partial results, and the last to finish (counters; nobody
+//     waits) adds them up in the blocks' order, so the result does not depend on timing.  Many parts are added in two
+//     levels, about the square root of them at a time.
 //   - fp32 queries (and probabilities) are split into two fp16 numbers, 22 bits together, with a product for each.  Two
 //     things that 16 bits do not show cost bits there: the matrix unit lines its products up by the operands' exponents, so that a
 //     subnormal's leading zeros are lost from the sum (1e-5 of the result), and it cuts sums off instead of rounding them.  So the codes
@@ -36,16 +38,21 @@ constexpr int WARPS = 4, THREADS = WARPS * 32;
 constexpr float M_NONE = -3.0e38f;               // reference before any score
 constexpr float M_SLACK = 8.f;                   // a score may pass the reference by this (log2)
 constexpr float V_SLACK = 64.f;                  // and a scale of V its norm by this: p * scale' <= 2^14 in fp16
+constexpr int UNIT = 4;                          // slices
+constexpr int HEAD = 3;                          // units
 
 template <int D, int NT, bool SPLIT> struct Cfg {
     static constexpr int ROWS = 8 * NT;
     static constexpr int SB = qp_kv_slice<D>::BYTES;
-    static constexpr int STAGES = D == 256 ? 4 : D == 128 ? 5 : 6;
+    static constexpr int SL = NT == 1 && !SPLIT && D < 256 ? 2 : 1;        // adjacent slices a warp takes at a time
+    static constexpr int STAGES = D == 256 ? 4 : D == 128 ? 5 : 8;         // slices in a warp's ring
     static constexpr int RING = WARPS * STAGES * SB;
     static constexpr int MERGE = WARPS * ROWS * (D + 2) * 4;
     static constexpr int SMEM = RING > MERGE ? RING : MERGE;
-    static constexpr int PER_SM = D == 256 ? 3 : NT == 2 || SPLIT ? 3 : 4;
+    static constexpr int PER_SM = D == 256 || NT == 2 || SPLIT ? 3 : 4;
+    static constexpr int PART = ROWS * (D + 2);                            // floats of a partial result
 };
+constexpr int MAX_PER_SM = 4, MAX_ROWS = 16;
 
 __device__ __forceinline__ float ex2(float x)
 {
@@ -100,6 +107,17 @@ __device__ __forceinline__ void copy16(char* dst, const char* src)
 __device__ __forceinline__ void copies_close() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+__device__ __forceinline__ qp_f2 mul2(qp_f2 a, qp_f2 b)
+{
+    qp_f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b)          // of non-negative numbers
+{
+    return (uint64_t)(a | b) >> 32 ? a / b : (int64_t)((unsigned)a / (unsigned)b);
+}
+
 template <int W>
 __device__ __forceinline__ void lds_words(const char* p, unsigned (&w)[W])
 {
@@ -116,9 +134,9 @@ __device__ __forceinline__ void lds_words(const char* p, unsigned (&w)[W])
 
 // What the batch asks for: sequence b's part.
 struct Seq {
-    int pos, n, row0;                            // first position, tokens, row of the first
+    int pos, n, row0, slot;                      // first position, tokens, row of the first
     int s0, s1;                                  // slices [s0, s1) hold the keys that some query sees
-    int units, tiles;                            // units of 64 tokens, query tiles
+    int units, tiles;                            // HEAD + units of 64 tokens, query tiles
     int64_t work;                                // units in all
 };
 
@@ -126,11 +144,12 @@ template <int ROWS>
 __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
 {
     Seq q;
+    q.pos = __ldg(a.rows.pos + b);
+    q.slot = qp_kv_slot(a.rows, b);
     q.row0 = qp_kv_start(a.rows, b);
     const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
     q.n = row1 - q.row0;
     if (q.n > a.max_new) q.n = a.max_new;
-    q.pos = __ldg(a.rows.pos + b);
     if (q.n <= 0 || q.pos < 0) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return q; }
     const int64_t most = (int64_t)a.pages.max_pages * a.pages.page_size;
     int64_t end = (int64_t)q.pos + q.n;
@@ -139,45 +158,45 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
     if (lo > end) lo = (int)end;
     q.s0 = lo / QP_KV_SLICE;
     q.s1 = (int)((end + QP_KV_SLICE - 1) / QP_KV_SLICE);
-    q.units = (q.s1 - q.s0 + WARPS - 1) / WARPS;
-    if (q.units < 1) q.units = 1;                                // an empty one still writes its rows
+    q.units = (q.s1 - q.s0 + UNIT - 1) / UNIT;
+    q.units = (q.units < 1 ? 1 : q.units) + HEAD;                // (an empty one still writes its rows)
     q.tiles = (int)(((int64_t)q.n * a.group + ROWS - 1) / ROWS);
     q.work = (int64_t)q.units * q.tiles * a.heads;
     return q;
 }
 
-// Block-wide: total work, or the sequence that unit `find` falls in and the work in front of it.
+// Sequences b0 .. b0 + THREADS - 1 into shared memory, with the work in front of each (base: in front of b0); returns the work
+// up to the last.
+struct Chunk {
+    int64_t before[THREADS + 1];
+    int64_t sum[WARPS];
+    int found;
+};
 template <int ROWS>
-__device__ __forceinline__ int64_t batch_work(const qp_kv_attn_args& a, int64_t find, int& at_b, int64_t& at_base, int64_t* sh)
+__device__ __forceinline__ int64_t load_chunk(const qp_kv_attn_args& a, int b0, int64_t base, Chunk& sh)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int64_t carry = 0;
-    for (int b0 = 0; b0 < a.rows.batch; b0 += THREADS) {
-        const int b = b0 + threadIdx.x;
-        const int64_t w = b < a.rows.batch ? seq_of<ROWS>(a, b).work : 0;
-        int64_t x = w;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = b0 + threadIdx.x;
+    Seq q;
+    q.work = 0;
+    if (b < a.rows.batch) q = seq_of<ROWS>(a, b);
+    int64_t x = q.work;
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
-            if (lane >= o) x += y;
-        }
-        __syncthreads();
-        if (lane == 31) sh[warp] = x;
-        __syncthreads();
-        int64_t total = 0, before = carry;
-#pragma unroll
-        for (int i = 0; i < WARPS; ++i) {
-            if (i == warp) before += total;
-            total += sh[i];
-        }
-        before += x - w;
-        if (find >= before && find < before + w) { sh[WARPS] = b; sh[WARPS + 1] = before; }
-        carry += total;
-        if (find >= 0 && find < carry) break;                    // uniform
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+        if (lane >= o) x += y;
     }
+    __syncthreads();                                             // nobody reads the chunk before this any more
+    if (lane == 31) sh.sum[warp] = x;
     __syncthreads();
-    if (find >= 0) { at_b = (int)sh[WARPS]; at_base = sh[WARPS + 1]; }
-    return carry;
+    int64_t front = base;
+#pragma unroll
+    for (int i = 0; i < WARPS; ++i) {
+        if (i < warp) front += sh.sum[i];
+        base += sh.sum[i];
+    }
+    sh.before[threadIdx.x + 1] = front + x;
+    if (threadIdx.x == 0) sh.before[0] = front;
+    return base;
 }
 
 // this lane's D / 4 elements of a query row
@@ -211,17 +230,100 @@ __device__ __forceinline__ void load_q(const float* p, bool vec, float (&e)[N])
         for (int i = 0; i < N; ++i) e[i] = __ldg(p + i);
     }
 }
-__device__ __forceinline__ void put_out(float* p, float v) { *p = v; }
-__device__ __forceinline__ void put_out(unsigned short* p, float v) { *p = qp_f32_to_bf16(v); }
+__device__ __forceinline__ void put_out(float* p, bool vec, const float (&v)[4])
+{
+    if (vec) *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = v[i];
+}
+__device__ __forceinline__ void put_out(unsigned short* p, bool vec, const float (&v)[4])
+{
+    unsigned short h[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) h[i] = qp_f32_to_bf16(v[i]);
+    if (vec) *reinterpret_cast<uint2*>(p) = make_uint2(h[0] | ((unsigned)h[1] << 16), h[2] | ((unsigned)h[3] << 16));
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = h[i];
+}
 
-// out row and lse of query row r of a tile's sequence
+// four elements of query row r of a sequence, from their weighted sum and the weights' sum l about the reference m
 template <typename T, int D>
-__device__ __forceinline__ void put_row(const qp_kv_attn_args& a, const Seq& q, int head, int r, int d, float o, float m, float l)
+__device__ __forceinline__ void put_row(const qp_kv_attn_args& a, const Seq& q, int head, int r, int d, float4 o, float m, float l)
 {
     const int token = q.row0 + r / a.group, h = head * a.group + r % a.group;
-    put_out(static_cast<T*>(a.out) + (int64_t)token * a.ot + (int64_t)h * a.oh + d, l == 0.f ? 0.f : o / l);
+    const float f = l == 0.f ? 0.f : 1.f;                        // (NaN stays NaN)
+    const float v[4] = {f == 0.f ? 0.f : o.x / l, f == 0.f ? 0.f : o.y / l, f == 0.f ? 0.f : o.z / l, f == 0.f ? 0.f : o.w / l};
+    put_out(static_cast<T*>(a.out) + (int64_t)token * a.ot + (int64_t)h * a.oh + d, a.out_vec, v);
     if (a.lse && d == 0)
         a.lse[(int64_t)token * a.q_heads + h] = l == 0.f ? -__int_as_float(0x7F800000) : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// Whether this block is the last of n to come here (the counter is at zero again then).  What the others wrote before is visible.
+__device__ __forceinline__ bool arrived(unsigned* count, int n, int& sh)
+{
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        sh = atomicAdd(count, 1u) == (unsigned)(n - 1);
+        if (sh) *count = 0u;
+    }
+    __syncthreads();
+    const bool last = sh != 0;
+    if (last) __threadfence();
+    return last;
+}
+
+// Adds n partial results: the first at place `at`, part i > 0 at place even + 2 * step * i; in that order.  Into `sum`, a partial
+// result again (it may be the first), or (null) into out.
+template <typename T, int D, int ROWS>
+__device__ __forceinline__ void add_parts(const qp_kv_attn_args& a, const Seq& q, int head, int tile, int rows, int at, int even,
+                                          int step, int n, float* sum, char* smem)
+{
+    constexpr int PART = ROWS * (D + 2);
+    auto part = [&](int i) { return a.part + (int64_t)(i ? even + 2 * step * i : at) * PART; };
+    float* f = reinterpret_cast<float*>(smem);                   // [n][ROWS] factors, then [ROWS] references and sums
+    float* tops = f + n * ROWS;
+    __syncthreads();                                             // shared memory is free
+    for (int i = threadIdx.x; i < n * rows; i += THREADS) {
+        const int p = i / rows, r = i - p * rows;
+        f[p * ROWS + r] = __ldcg(part(p) + ROWS * D + r);
+    }
+    __syncthreads();
+    for (int r = threadIdx.x >> 5; r < rows; r += WARPS) {       // a warp to a row
+        const int lane = threadIdx.x & 31;
+        float top = M_NONE;
+        for (int p = lane; p < n; p += 32) top = fmaxf(top, f[p * ROWS + r]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+        float l = 0.f;
+        for (int p = lane; p < n; p += 32) {
+            const float w = ex2(f[p * ROWS + r] - top);
+            f[p * ROWS + r] = w;
+            l = fmaf(w, __ldcg(part(p) + ROWS * D + ROWS + r), l);
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
+        if (lane == 0) { tops[r] = top; tops[ROWS + r] = l; }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
+        const int r = i / (D / 4), d = 4 * (i % (D / 4));
+        float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int p = 0; p < n; ++p) {
+            const float4 y = __ldcg(reinterpret_cast<const float4*>(part(p) + r * D + d));
+            const float w = f[p * ROWS + r];
+            so.x = fmaf(y.x, w, so.x); so.y = fmaf(y.y, w, so.y); so.z = fmaf(y.z, w, so.z); so.w = fmaf(y.w, w, so.w);
+        }
+        if (!sum) {
+            put_row<T, D>(a, q, head, tile * ROWS + r, d, so, tops[r], tops[ROWS + r]);
+        } else {
+            __stcg(reinterpret_cast<float4*>(sum + r * D + d), so);
+            if (d == 0) { __stcg(sum + ROWS * D + r, tops[r]); __stcg(sum + ROWS * D + ROWS + r, tops[ROWS + r]); }
+        }
+    }
 }
 
 template <int D, int NT, bool SPLIT>
@@ -230,25 +332,26 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     using C = Cfg<D, NT, SPLIT>;
     using S = qp_kv_slice<D>;
     using T = typename std::conditional<SPLIT, float, unsigned short>::type;
-    constexpr int ROWS = C::ROWS, SB = C::SB, STAGES = C::STAGES;
+    constexpr int ROWS = C::ROWS, SB = C::SB, STAGES = C::STAGES, SL = C::SL;
     constexpr int KW = D / 32, VW = D / 64;                      // words of 8 codes a lane holds of a K row, of a V row
     constexpr int QB = 4 * KW;                                   // operand registers of a query tile
     constexpr unsigned M0 = 0x000F000Fu, M1 = 0x00F000F0u;
     extern __shared__ __align__(16) char smem[];
-    __shared__ int64_t sh_work[WARPS + 2];
+    __shared__ Chunk chunk;
     __shared__ int sh_ok[WARPS][STAGES];
     __shared__ int sh_last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = lane >> 2, j = lane & 3;
 
-    int b = 0;
-    int64_t base = 0;
-    const int64_t W = batch_work<ROWS>(a, -1, b, base, sh_work);
-    int64_t blocks = gridDim.x;
-    if (blocks > W) blocks = W;
+    int b0 = 0;
+    int64_t base = 0, upto = load_chunk<ROWS>(a, 0, 0, chunk), W = upto;
+    for (int c = THREADS; c < a.rows.batch; c += THREADS) W = load_chunk<ROWS>(a, c, W, chunk);
+    const int64_t blocks = (int64_t)gridDim.x < W ? (int64_t)gridDim.x : W;
     if ((int64_t)blockIdx.x >= blocks) return;
-    const int64_t begin = blockIdx.x * W / blocks, end = (blockIdx.x + 1ll) * W / blocks;
-    __syncthreads();
-    batch_work<ROWS>(a, begin, b, base, sh_work);
+    const int64_t begin = quotient(blockIdx.x * W, blocks), end = quotient((blockIdx.x + 1ll) * W, blocks);
+    if (a.rows.batch > THREADS) {                                // back to the chunk that the run begins in
+        upto = load_chunk<ROWS>(a, 0, 0, chunk);
+        while (upto <= begin) { base = upto; upto = load_chunk<ROWS>(a, b0 += THREADS, base, chunk); }
+    }
 
     char* ring = smem + warp * (STAGES * SB);
     // rows of the slice behind operand row n: n and n + 8 with the middle pairs crossed, so that the four rows a quarter of the lanes
@@ -258,21 +361,58 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     bool flag = false;
 
     for (int64_t u = begin; u < end;) {
-        Seq q = seq_of<ROWS>(a, b);
-        while (u >= base + q.work) {                             // on to the next sequence with work
-            base += q.work;
-            q = seq_of<ROWS>(a, ++b);
-        }
-        const int64_t local = u - base, item = local / q.units;
-        const int u0 = (int)(local - item * q.units);
-        const int u1 = (int)(q.units - u0 < end - u ? q.units : u0 + (end - u));
-        const int head = (int)(item / q.tiles), tile = (int)(item - (int64_t)head * q.tiles);
+        while (u >= upto) { base = upto; upto = load_chunk<ROWS>(a, b0 += THREADS, base, chunk); }
+        __syncthreads();
+        if (u >= chunk.before[threadIdx.x] && u < chunk.before[threadIdx.x + 1]) chunk.found = threadIdx.x;
+        __syncthreads();
+        const Seq q = seq_of<ROWS>(a, b0 + chunk.found);
+        const int64_t front = chunk.before[chunk.found], local = u - front, item = quotient(local, q.units);
+        const int g0 = (int)(local - item * q.units), g1 = (int)(q.units - g0 < end - u ? q.units : g0 + (end - u));
+        const int64_t here = u;
+        u += g1 - g0;
+        const int u0 = g0 > HEAD ? g0 - HEAD : 0, u1 = g1 - HEAD;
+        if (u1 <= u0) continue;                                  // nothing but the item's head
+        const int head = (int)quotient(item, q.tiles), tile = (int)(item - (int64_t)head * q.tiles);
         const int rows = q.n * a.group - tile * ROWS < ROWS ? q.n * a.group - tile * ROWS : ROWS;   // of the tile
-        const int slot = qp_kv_slot(a.rows, b);
+
+        // ---- the warp's slices, SL adjacent ones at a time: first + SL * WARPS * k + h
+        const int first = q.s0 + UNIT * u0 + SL * warp;
+        const int stop = q.s1 < q.s0 + UNIT * u1 ? q.s1 : q.s0 + UNIT * u1;
+        const int count = first < stop ? (stop - first + SL * WARPS - 1) / (SL * WARPS) : 0;
+        int64_t place = -1;                                      // lane i: where the warp's slice number 32 * k + i lies
+        auto look_up = [&](int k) {
+            const int s = first + SL * WARPS * ((32 * k + lane) / SL) + (SL == 2 ? lane & 1 : 0);
+            place = -1;
+            if (s < stop) {
+                const int p = s / a.slices;
+                const int page = qp_kv_page(a.pages, q.slot, p * a.pages.page_size);
+                if (page >= 0) place = (((int64_t)page * a.heads + head) * a.slices + (s - p * a.slices)) * SB;
+                else flag = true;
+            }
+        };
+        int put = 0, take = 0;                                   // places in the ring
+        auto issue = [&](int i) {                                // the warp's slice number i
+            if (i < count * SL) {
+                if ((i & 31) == 0) look_up(i >> 5);
+                const int64_t from = __shfl_sync(0xFFFFFFFFu, place, i & 31);
+                if (lane == 0) sh_ok[warp][put] = from >= 0;
+                if (from >= 0) {
+                    char* to = ring + put * SB + lane * 16;
+                    const char* src = a.pool + from + lane * 16;
+#pragma unroll
+                    for (int c = 0; c < SB / 512; ++c) copy16(to + 512 * c, src + 512 * c);
+                    if (SB % 512 && lane < SB % 512 / 16) copy16(to + SB / 512 * 512, src + SB / 512 * 512);
+                }
+                put = put + 1 == STAGES ? 0 : put + 1;
+            }
+            copies_close();
+        };
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i) issue(i);
 
         // ---- queries: operand registers and, per column, the factors of a score
         unsigned qb[NT][QB], ql[SPLIT ? NT : 1][SPLIT ? QB : 1];
-        float kf[NT][2], qs[NT][2];
+        qp_f2 kf[NT], qs[NT];
         int hi[NT][2];                                           // last key that the column's query sees
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -313,10 +453,10 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                 }
             }
             const float my_kf = a.scale_log2 / norm * (SPLIT ? 1.f : 16777216.f), my_qs = bad ? __int_as_float(0x7FC00000) : sum * a.scale_log2;
+            kf[t] = qp_pack2(__shfl_sync(0xFFFFFFFFu, my_kf, 8 * j), __shfl_sync(0xFFFFFFFFu, my_kf, 8 * j + 4));
+            qs[t] = qp_pack2(__shfl_sync(0xFFFFFFFFu, my_qs, 8 * j), __shfl_sync(0xFFFFFFFFu, my_qs, 8 * j + 4));
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                kf[t][c] = __shfl_sync(0xFFFFFFFFu, my_kf, 4 * (2 * j + c));
-                qs[t][c] = __shfl_sync(0xFFFFFFFFu, my_qs, 4 * (2 * j + c));
                 int rc = 8 * t + 2 * j + c;
                 rc = rc < rows ? rc : rows - 1;
                 hi[t][c] = q.pos + (tile * ROWS + rc) / a.group;
@@ -329,64 +469,42 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         const int held = q.pos + q.n;                            // tokens behind are not written yet
 
         float o[NT][4 * VW][4];
-        float m[NT][2], l[NT][2], lv[NT][2], vn = 1.2676506e30f; // 2^100
+        qp_f2 mn[NT], l[NT], lv[NT];                             // the reference, negated; sums of p and of p * lo'
+        float vn = 1.2676506e30f;                                // 2^100
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int i = 0; i < 4 * VW; ++i)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) o[t][i][c] = 0.f;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) { m[t][c] = M_NONE; l[t][c] = lv[t][c] = 0.f; }
+            mn[t] = qp_pack2(-M_NONE, -M_NONE);
+            l[t] = lv[t] = qp_pack2(0.f, 0.f);
         }
 
-        // ---- the warp's slices: first, first + 4, ...
-        const int first = q.s0 + WARPS * u0 + warp;
-        int count = (q.s1 - first + WARPS - 1) / WARPS;
-        count = count < u1 - u0 ? count : u1 - u0;               // may be negative: none
-        int64_t place = -1;                                      // lane i: where slice 32 * k + i of the warp lies
-        auto look_up = [&](int k) {
-            const int it = 32 * k + lane;
-            place = -1;
-            if (it < count) {
-                const int s = first + WARPS * it, p = s / a.slices;
-                const int page = qp_kv_page(a.pages, slot, p * a.pages.page_size);
-                if (page >= 0) place = (((int64_t)page * a.heads + head) * a.slices + (s - p * a.slices)) * SB;
-                else flag = true;
-            }
-        };
-        auto issue = [&](int it) {
-            if (it < count) {
-                if ((it & 31) == 0) look_up(it >> 5);
-                const int64_t from = __shfl_sync(0xFFFFFFFFu, place, it & 31);
-                char* to = ring + (it % STAGES) * SB + lane * 16;
-                if (lane == 0) sh_ok[warp][it % STAGES] = from >= 0;
-                if (from >= 0) {
-                    const char* src = a.pool + from + lane * 16;
-#pragma unroll
-                    for (int i = 0; i < SB / 512; ++i) copy16(to + 512 * i, src + 512 * i);
-                    if (SB % 512 && lane < SB % 512 / 16) copy16(to + SB / 512 * 512, src + SB / 512 * 512);
-                }
-            }
-            copies_close();
-        };
-#pragma unroll
-        for (int i = 0; i < STAGES - 1; ++i) issue(i);
         for (int it = 0; it < count; ++it) {
-            copies_wait<STAGES - 2>();
+            copies_wait<STAGES - SL>();
             __syncwarp();
-            issue(it + STAGES - 1);                              // into the stage of the round before
-            const int stage = it % STAGES;
-            if (!sh_ok[warp][stage]) continue;
-            const char* x = ring + stage * SB;
-            const int t0 = (first + WARPS * it) * QP_KV_SLICE;
+            const int t0 = (first + SL * WARPS * it) * QP_KV_SLICE;
+            const char* at[SL];
+            bool ok[SL], all = t0 >= all_lo && t0 + SL * QP_KV_SLICE <= all_hi;
+#pragma unroll
+            for (int i = 0; i < SL; ++i) {
+                at[i] = ring + take * SB;
+                ok[i] = sh_ok[warp][take] != 0;
+                all = all && ok[i];
+                take = take + 1 == STAGES ? 0 : take + 1;
+            }
 
-            float s[NT][4];
+            qp_f2 s[SL][NT][2];                                  // scores, in log2: of operand rows n and n + 8, two queries each
+            float2 vq[SL][2];
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int i = 0; i < SL; ++i) {
+                const char* x = at[i];
+                float raw[NT][4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) s[t][c] = 0.f;
-            {
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) raw[t][c] = 0.f;
                 unsigned ka[KW], kb[KW];
                 lds_words(x + tok * S::ROW + j * (D / 8), ka);
                 lds_words(x + (8 + tok) * S::ROW + j * (D / 8), kb);
@@ -404,55 +522,60 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                             mma(x4, c0, c1, c2, c3, qb[t][4 * w], qb[t][4 * w + 1]);
                             mma(x4, e0, e1, e2, e3, qb[t][4 * w + 2], qb[t][4 * w + 3]);
 #pragma unroll
-                            for (int c = 0; c < 4; ++c) s[t][c] += x4[c];
+                            for (int c = 0; c < 4; ++c) raw[t][c] += x4[c];
                         } else {
-                            mma(s[t], c0, c1, c2, c3, qb[t][4 * w], qb[t][4 * w + 1]);
-                            mma(s[t], e0, e1, e2, e3, qb[t][4 * w + 2], qb[t][4 * w + 3]);
+                            mma(raw[t], c0, c1, c2, c3, qb[t][4 * w], qb[t][4 * w + 1]);
+                            mma(raw[t], e0, e1, e2, e3, qb[t][4 * w + 2], qb[t][4 * w + 3]);
                         }
                     }
                 }
-            }
-            float2 kq[2], vq[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                kq[h] = *reinterpret_cast<const float2*>(x + S::KQ + (8 * h + tok) * 8);
-                vq[h] = *reinterpret_cast<const float2*>(x + S::VQ + (8 * h + tok) * 8);
-            }
-            const bool whole = t0 >= all_lo && t0 + QP_KV_SLICE <= all_hi;
-            if (!whole) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)                      // rows that were never written may hold anything
-                    if (t0 + 8 * h + tok >= held) kq[h] = vq[h] = make_float2(0.f, 0.f);
-            }
-            if constexpr (SPLIT) {                               // the codes are less 8: lo is the value of code 8
+                float2 kq[2];
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    kq[h].x = fmaf(8.f, kq[h].y, kq[h].x);
-                    vq[h].x = fmaf(8.f, vq[h].y, vq[h].x);
+                    kq[h] = *reinterpret_cast<const float2*>(x + S::KQ + (8 * h + tok) * 8);
+                    vq[i][h] = *reinterpret_cast<const float2*>(x + S::VQ + (8 * h + tok) * 8);
+                    // rows that were never written, or not copied, may hold anything
+                    if (!all && (!ok[i] || t0 + 16 * i + 8 * h + tok >= held)) kq[h] = vq[i][h] = make_float2(0.f, 0.f);
+                    if constexpr (SPLIT) {                       // the codes are less 8: lo is the value of code 8
+                        kq[h].x = fmaf(8.f, kq[h].y, kq[h].x);
+                        vq[i][h].x = fmaf(8.f, vq[i][h].y, vq[i][h].x);
+                    }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+                        s[i][t][h] = qp_fma2(mul2(qp_pack2(raw[t][2 * h], raw[t][2 * h + 1]), qp_pack2(kq[h].y, kq[h].y)), kf[t],
+                                             mul2(qp_pack2(kq[h].x, kq[h].x), qs[t]));
                 }
             }
-            // scores, in log2
-            bool raise = vq[0].y * vn > V_SLACK || vq[1].y * vn > V_SLACK;
+            if (!all) {
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+                for (int i = 0; i < SL; ++i)
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    s[t][c] = fmaf(s[t][c] * kq[c >> 1].y, kf[t][c & 1], kq[c >> 1].x * qs[t][c & 1]);
-            if (!whole) {
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                        for (int h = 0; h < 2; ++h) {
+                            float y[2];
+                            qp_unpack2(s[i][t][h], y[0], y[1]);
+                            const int key = t0 + 16 * i + 8 * h + tok;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        const int key = t0 + 8 * (c >> 1) + tok;
-                        if (key > hi[t][c & 1] || (a.window > 0 && key <= hi[t][c & 1] - a.window)) s[t][c] = -__int_as_float(0x7F800000);
-                    }
+                            for (int c = 0; c < 2; ++c)
+                                if (!ok[i] || key > hi[t][c] || (a.window > 0 && key <= hi[t][c] - a.window)) y[c] = -__int_as_float(0x7F800000);
+                            s[i][t][h] = qp_pack2(y[0], y[1]);
+                        }
             }
+            float over = -1.f, vmax = 0.f;                       // how far the scores pass their references, the scales their norm
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
+            for (int i = 0; i < SL; ++i)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) raise = raise || s[t][c] > m[t][c & 1] + M_SLACK;
-            if (__any_sync(0xFFFFFFFFu, raise)) {                // rare: new references
-                float vmax = fmaxf(vq[0].y, vq[1].y), f[NT][2];
+                for (int h = 0; h < 2; ++h) {
+                    vmax = fmaxf(vmax, vq[i][h].y);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) {
+                        float y0, y1;
+                        qp_unpack2(qp_add2(s[i][t][h], mn[t]), y0, y1);
+                        over = qp_max3(over, y0, y1);
+                    }
+                }
+            if (__any_sync(0xFFFFFFFFu, over > M_SLACK || vmax * vn > V_SLACK)) {      // rare: new references
 #pragma unroll
                 for (int o2 = 4; o2 < 32; o2 <<= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, o2));
                 float back = 1.f;
@@ -464,47 +587,59 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                     vn = next;
                 }
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) {
+                    float top[2] = {M_NONE, M_NONE}, old[2], f[2];
+                    qp_unpack2(mn[t], old[0], old[1]);
+#pragma unroll
+                    for (int i = 0; i < SL; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float y0, y1;
+                            qp_unpack2(s[i][t][h], y0, y1);
+                            top[0] = fmaxf(top[0], y0);
+                            top[1] = fmaxf(top[1], y1);
+                        }
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        float top = fmaxf(s[t][c], s[t][c + 2]);
 #pragma unroll
-                        for (int o2 = 4; o2 < 32; o2 <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o2));
-                        const float next = fmaxf(m[t][c], top);
-                        f[t][c] = ex2(m[t][c] - next);
-                        m[t][c] = next;
-                        l[t][c] *= f[t][c];
-                        lv[t][c] *= f[t][c];
-                        f[t][c] *= back;
+                        for (int o2 = 4; o2 < 32; o2 <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xFFFFFFFFu, top[c], o2));
+                        top[c] = fmaxf(-old[c], top[c]);
+                        f[c] = ex2(-old[c] - top[c]);
                     }
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
+                    mn[t] = qp_pack2(-top[0], -top[1]);
+                    l[t] = mul2(l[t], qp_pack2(f[0], f[1]));
+                    lv[t] = mul2(lv[t], qp_pack2(f[0], f[1]));
+                    f[0] *= back;
+                    f[1] *= back;
 #pragma unroll
                     for (int i = 0; i < 4 * VW; ++i)
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) o[t][i][c] *= f[t][c & 1];
-            }
-            // probabilities; times V's scale they are the second product's operand
-            unsigned pb[NT][2], pl[SPLIT ? NT : 1][2];
-            const float vs[2] = {vq[0].y * vn, vq[1].y * vn};
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float p0 = ex2(s[t][2 * h] - m[t][0]), p1 = ex2(s[t][2 * h + 1] - m[t][1]);
-                    l[t][0] += p0;
-                    l[t][1] += p1;
-                    lv[t][0] = fmaf(p0, vq[h].x, lv[t][0]);
-                    lv[t][1] = fmaf(p1, vq[h].x, lv[t][1]);
-                    const float w0 = p0 * vs[h], w1 = p1 * vs[h];
-                    const unsigned x2 = half2_of(w0, w1);
-                    pb[t][h] = transpose8(x2);
-                    if constexpr (SPLIT) pl[t][h] = transpose8(half2_of(w0 - half_lo(x2), w1 - half_hi(x2)));
+                        for (int c = 0; c < 4; ++c) o[t][i][c] *= f[c & 1];
                 }
-            // out^T += V^T P^T
-            {
+            }
+#pragma unroll
+            for (int i = 0; i < SL; ++i) {
+                // probabilities; times V's scale they are the second product's operand
+                unsigned pb[NT][2], pl[SPLIT ? NT : 1][2];
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        float p0, p1;
+                        qp_unpack2(qp_add2(s[i][t][h], mn[t]), p0, p1);
+                        const qp_f2 p = qp_pack2(ex2(p0), ex2(p1));
+                        l[t] = qp_add2(l[t], p);
+                        lv[t] = qp_fma2(p, qp_pack2(vq[i][h].x, vq[i][h].x), lv[t]);
+                        const float vs = vq[i][h].y * vn;
+                        float w0, w1;
+                        qp_unpack2(mul2(p, qp_pack2(vs, vs)), w0, w1);
+                        const unsigned x2 = half2_of(w0, w1);
+                        pb[t][h] = transpose8(x2);
+                        if constexpr (SPLIT) pl[t][h] = transpose8(half2_of(w0 - half_lo(x2), w1 - half_hi(x2)));
+                    }
+                // out^T += V^T P^T
                 unsigned w0[VW], w1[VW], w2[VW], w3[VW];
-                const char* v = x + S::V + n * (D / 16);
+                const char* v = at[i] + S::V + n * (D / 16);
                 lds_words(v + v0 * S::ROW, w0);
                 lds_words(v + v1 * S::ROW, w1);
                 lds_words(v + (8 + v0) * S::ROW, w2);
@@ -533,6 +668,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                         }
                     }
             }
+            __syncwarp();                                        // all lanes have read: the places are filled again
+#pragma unroll
+            for (int i = 0; i < SL; ++i) issue(SL * it + STAGES + i);
         }
         copies_wait<0>();
         __syncthreads();                                         // the ring is free: it takes the warps' results
@@ -543,81 +681,84 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         float* ml = mm + WARPS * ROWS;
         const float un = 1.f / vn;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int t = 0; t < NT; ++t) {
+            float sl[2], sv[2], mc[2];
+            qp_unpack2(l[t], sl[0], sl[1]);
+            qp_unpack2(lv[t], sv[0], sv[1]);
+            qp_unpack2(mn[t], mc[0], mc[1]);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                float sl = l[t][c], sv = lv[t][c];
 #pragma unroll
                 for (int o2 = 4; o2 < 32; o2 <<= 1) {
-                    sl += __shfl_xor_sync(0xFFFFFFFFu, sl, o2);
-                    sv += __shfl_xor_sync(0xFFFFFFFFu, sv, o2);
+                    sl[c] += __shfl_xor_sync(0xFFFFFFFFu, sl[c], o2);
+                    sv[c] += __shfl_xor_sync(0xFFFFFFFFu, sv[c], o2);
                 }
                 const int r = 8 * t + 2 * j + c;
-                if (n == 0) { mm[warp * ROWS + r] = m[t][c]; ml[warp * ROWS + r] = sl; }
+                if (n == 0) { mm[warp * ROWS + r] = -mc[c]; ml[warp * ROWS + r] = sl[c]; }
                 float* row = mo + (warp * ROWS + r) * D + n * (D / 8);
 #pragma unroll
-                for (int i = 0; i < 4 * VW; ++i) {               // tile i: elements e and e + 2 of word i / 4
-                    const float f = (i & 1 ? 0.0625f : 1.f) * (SPLIT ? 1.f : 16777216.f);
-                    const int e = 8 * (i >> 2) + 4 * ((i >> 1) & 1) + (i & 1);
-                    row[e] = fmaf(o[t][i][c] * un, f, sv);
-                    row[e + 2] = fmaf(o[t][i][c + 2] * un, f, sv);
+                for (int i = 0; i < 4 * VW; i += 2) {            // tiles i and i + 1: elements e, e + 2 and e + 1, e + 3 of word i / 4
+                    constexpr float f = SPLIT ? 1.f : 16777216.f;
+                    *reinterpret_cast<float4*>(row + 8 * (i >> 2) + 4 * ((i >> 1) & 1)) =
+                        make_float4(fmaf(o[t][i][c] * un, f, sv[c]), fmaf(o[t][i + 1][c] * un, f * 0.0625f, sv[c]),
+                                    fmaf(o[t][i][c + 2] * un, f, sv[c]), fmaf(o[t][i + 1][c + 2] * un, f * 0.0625f, sv[c]));
                 }
             }
+        }
         __syncthreads();
-        const bool split = u0 > 0 || u1 < q.units;
-        float* part = a.part + ((int64_t)blockIdx.x * 2 + (u == begin ? 0 : 1)) * (ROWS * (D + 2));
-        for (int i = threadIdx.x; i < rows * D; i += THREADS) {
-            const int r = i / D, d = i % D;
+        const bool split = u0 > 0 || u1 < q.units - HEAD;
+        const int64_t i0 = here - g0;                            // the item's first unit; its blocks:
+        int c0 = 0, c1 = 0, at = 0;
+        if (split) {
+            c0 = (int)quotient((i0 + HEAD + 1) * blocks - 1, W);
+            c1 = (int)quotient((i0 + q.units) * blocks - 1, W);
+            // a block's part of an item is its first if the item began in front of it or with it
+            at = 2 * (int)blockIdx.x + (here == begin ? 0 : 1);
+        }
+        float* part = a.part + (int64_t)at * C::PART;
+        for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
+            const int r = i / (D / 4), d = 4 * (i % (D / 4));
             float top = mm[r];
 #pragma unroll
             for (int w = 1; w < WARPS; ++w) top = fmaxf(top, mm[w * ROWS + r]);
-            float so = 0.f, sl = 0.f;
+            float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
+            float sl = 0.f;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
                 const float f = ex2(mm[w * ROWS + r] - top);
-                so = fmaf(mo[(w * ROWS + r) * D + d], f, so);
+                const float4 y = *reinterpret_cast<const float4*>(mo + (w * ROWS + r) * D + d);
+                so.x = fmaf(y.x, f, so.x); so.y = fmaf(y.y, f, so.y); so.z = fmaf(y.z, f, so.z); so.w = fmaf(y.w, f, so.w);
                 sl = fmaf(ml[w * ROWS + r], f, sl);
             }
             if (!split) {
                 put_row<T, D>(a, q, head, tile * ROWS + r, d, so, top, sl);
             } else {
-                __stcg(part + r * D + d, so);
+                __stcg(reinterpret_cast<float4*>(part + r * D + d), so);
                 if (d == 0) { __stcg(part + ROWS * D + r, top); __stcg(part + ROWS * D + ROWS + r, sl); }
             }
         }
         if (split) {
-            // blocks of this item: those of units i0 and i0 + units - 1, and all between
-            const int64_t i0 = base + item * q.units;
-            const int c0 = (int)(((i0 + 1) * blocks - 1) / W), c1 = (int)(((i0 + q.units) * blocks - 1) / W);
-            __threadfence();
-            __syncthreads();
-            if (threadIdx.x == 0) {
-                const unsigned done = atomicAdd(a.count + c0, 1u);
-                sh_last = done == (unsigned)(c1 - c0);
-                if (sh_last) a.count[c0] = 0u;
+            // the parts of blocks c0 .. c1, `step` of them to a group; the group's sum takes the place of its first part
+            const int parts = c1 - c0 + 1, first_at = 2 * c0 + (quotient(c0 * W, blocks) < i0 ? 1 : 0);
+            int step = parts;
+            if (parts > 8) {
+                step = 4;
+                while (step * step < parts) ++step;
             }
-            __syncthreads();
-            if (sh_last) {
-                __threadfence();
-                for (int i = threadIdx.x; i < rows * D; i += THREADS) {
-                    const int r = i / D, d = i % D;
-                    // a block's part of this item is its first unless it began in front of the item
-                    const float* p1 = a.part + ((int64_t)c0 * 2 + (c0 * W / blocks < i0 ? 1 : 0)) * (ROWS * (D + 2));
-                    float top = __ldcg(p1 + ROWS * D + r);
-                    for (int c = c0 + 1; c <= c1; ++c) top = fmaxf(top, __ldcg(a.part + (int64_t)c * 2 * (ROWS * (D + 2)) + ROWS * D + r));
-                    float so = 0.f, sl = 0.f;
-                    for (int c = c0; c <= c1; ++c) {
-                        const float* p = c == c0 ? p1 : a.part + (int64_t)c * 2 * (ROWS * (D + 2));
-                        const float f = ex2(__ldcg(p + ROWS * D + r) - top);
-                        so = fmaf(__ldcg(p + r * D + d), f, so);
-                        sl = fmaf(__ldcg(p + ROWS * D + ROWS + r), f, sl);
-                    }
-                    put_row<T, D>(a, q, head, tile * ROWS + r, d, so, top, sl);
-                }
+            const int group = ((int)blockIdx.x - c0) / step, groups = (parts + step - 1) / step;
+            const int gc = c0 + group * step, gn = parts - group * step < step ? parts - group * step : step;
+            const int g_at = group ? 2 * gc : first_at;
+            float* sum = a.part + (int64_t)g_at * C::PART;
+            bool mine = arrived(a.count + g_at, gn, sh_last);
+            if (mine && groups == 1) {
+                add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, 1, parts, nullptr, smem);
+            } else if (mine) {
+                add_parts<T, D, ROWS>(a, q, head, tile, rows, g_at, 2 * gc, 1, gn, sum, smem);
+                mine = arrived(a.count + QP_KV_COUNTERS / 2 + first_at, groups, sh_last);
+                if (mine) add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, step, groups, nullptr, smem);
             }
         }
         __syncthreads();                                         // shared memory is free for the next part
-        u += u1 - u0;
     }
     if (flag) atomicOr(a.status, QP_DEV_KV_RANGE);
 }
@@ -645,8 +786,6 @@ Launch choose(int dim, bool f32, int64_t rows)
     if (rows > 8) return dim == 64 ? launch_of<64, 2, false>() : launch_of<128, 2, false>();
     return dim == 64 ? launch_of<64, 1, false>() : launch_of<128, 1, false>();
 }
-
-constexpr int MAX_PER_SM = 4, MAX_ROWS = 16;
 
 }  // namespace
 
@@ -698,12 +837,13 @@ extern "C" int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, co
     a.out = d_out; a.ot = out_token_stride; a.oh = out_head_stride;
     a.lse = d_lse;
     a.vec = (((uintptr_t)d_q & 15u) | (uintptr_t)(((q_token_stride | q_head_stride) * es) & 15)) == 0;
+    a.out_vec = (((uintptr_t)d_out & (uintptr_t)(4 * es - 1)) | (uintptr_t)(((out_token_stride | out_head_stride) * es) & (4 * es - 1))) == 0;
     a.count = static_cast<unsigned*>(h_plan->d_work);
     a.part = reinterpret_cast<float*>(a.count + QP_KV_COUNTERS);
     a.status = ctx->d_status;
     const Launch f = choose(c->head_dim, dtype == QP_F32, (int64_t)a.max_new * group);
     const int grid = ctx->sm_count * f.per_sm;
-    if (grid > QP_KV_COUNTERS) return qp_fail(ctx, QP_ERR_INVALID_ARG, "device with more SMs than the workspace has counters for");
+    if (2 * grid > QP_KV_COUNTERS / 2) return qp_fail(ctx, QP_ERR_INVALID_ARG, "device with more SMs than the workspace has counters for");
     if (ctx->device >= QP_KV_MAX_DEVICES || !f.ready[ctx->device]) {
         if (cudaFuncSetAttribute(f.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, f.smem) != cudaSuccess)
             return qp_check_launch(ctx, "qp_kv_attention (shared memory)");

@@ -6,7 +6,7 @@
 #include "qp_kv.cuh"
 
 constexpr int QP_KV_MAX_DEVICES = 64;
-constexpr int QP_KV_COUNTERS = 4096;             // of a plan's workspace: one for each block
+constexpr int QP_KV_COUNTERS = 4096;             // of a plan's workspace: two levels, two for each block
 
 struct qp_kv_attn_args {
     qp_kv_rows rows;
@@ -20,7 +20,7 @@ struct qp_kv_attn_args {
     void* out;
     int64_t ot, oh;
     float* lse;
-    bool vec;                                    // 16-byte loads of q
+    bool vec, out_vec;                           // 16-byte loads of q; stores of four elements
     unsigned* count;
     float* part;
     unsigned* status;
