@@ -107,7 +107,7 @@ class QuantPipeError(RuntimeError):
 
 
 _lib = None
-_call = _call64 = _tensor_in = None                 # of _qpcall, once load() has run
+_call = _call64 = _tensor_in = _rows_of = _ints_of = None    # of _qpcall, once load() has run
 _addr: dict = {}                                    # numbers of the entry points bound for it
 
 
@@ -211,14 +211,15 @@ def load() -> C.CDLL:
 
 
 def _load_call_path(L: C.CDLL) -> None:
-    global _call, _call64, _tensor_in
+    global _call, _call64, _tensor_in, _rows_of, _ints_of
     try:
         from . import _qpcall
     except ImportError as e:
         raise RuntimeError("_qpcall is missing: build it with `python -m paper_2211_04515_b200.build` "
                            "(there is no CPU fallback)") from e
-    _qpcall.setup(torch.float32, torch.bfloat16)
+    _qpcall.setup(torch.float32, torch.bfloat16, torch.int32)
     _call, _call64, _tensor_in = _qpcall.call, _qpcall.call64, _qpcall.tensor_in
+    _rows_of, _ints_of = _qpcall.rows, _qpcall.ints
     for name in EXPORTS:
         fn = getattr(L, name)
         if fn.argtypes and C.c_double not in fn.argtypes:
@@ -374,14 +375,13 @@ def qp_kv_slice_bytes(head_dim: int) -> int:
     return int(load().qp_kv_slice_bytes(head_dim))
 
 
-def _ints(t: torch.Tensor, what: str, device, n: int | None = None) -> torch.Tensor:
-    if not (isinstance(t, torch.Tensor) and t.dtype == torch.int32 and t.is_cuda and t.is_contiguous()):
-        raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} must be a contiguous int32 CUDA tensor")
-    if device is not None and t.device != device:
-        raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} is on another device")
-    if n is not None and t.numel() != n:
-        raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} must have {n} entries")
-    return t
+def _ints(t: torch.Tensor, what: str, index: int, n: int | None = None) -> int:
+    """Elements of a contiguous int32 tensor on that device."""
+    got = _ints_of(t, index)
+    if got < 0 or (n is not None and got != n):
+        raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} must be a contiguous int32 tensor on cuda:{index}"
+                                                 + ("" if n is None else f" of {n} entries"))
+    return got
 
 
 class KVCache:
@@ -399,7 +399,8 @@ class KVCache:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "pool must be a CUDA tensor [layers, pages, heads, page_size / 16, "
                                                      f"{slice_bytes}] of bytes, each layer contiguous")
         layers, pages, heads, slices, _ = pool.shape
-        _ints(table, "table", pool.device), _ints(lens, "lens", pool.device), _ints(refs, "refs", pool.device, pages)
+        self._index = pool.get_device()
+        _ints(table, "table", self._index), _ints(lens, "lens", self._index), _ints(refs, "refs", self._index, pages)
         if table.dim() != 2 or lens.numel() != table.shape[0]:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "table must be [slots, pages of a sequence] and lens [slots]")
         self.pool, self.table, self.lens, self.refs, self.head_dim = pool, table, lens, refs, head_dim
@@ -430,12 +431,13 @@ class KVBatch:
 
     def __init__(self, pos: torch.Tensor, slots: torch.Tensor | None = None, start: torch.Tensor | None = None,
                  tokens: int | None = None, max_new: int | None = None):
-        _ints(pos, "pos", None)
-        n = pos.numel()
+        load()
+        self._index = pos.get_device()
+        n = _ints(pos, "pos", self._index)
         if slots is not None:
-            _ints(slots, "slots", pos.device, n)
+            _ints(slots, "slots", self._index, n)
         if start is not None:
-            _ints(start, "start", pos.device, n + 1)
+            _ints(start, "start", self._index, n + 1)
             if tokens is None or max_new is None:
                 raise QuantPipeError(QP_ERR_INVALID_ARG, "tokens and max_new are needed with start")
         self.pos, self.slots, self.start = pos, slots, start
@@ -450,6 +452,7 @@ class KVAttention:
 
     def __init__(self, work: torch.Tensor, q_heads: int, window: int, scale: float):
         self.work, self.q_heads, self.window, self.scale = work, q_heads, window, scale
+        self._index = work.get_device()
         self._desc = KVAttentionDesc(work.data_ptr(), work.nbytes, q_heads, window, scale, 0)
         self._at = C.addressof(self._desc)
 
@@ -719,19 +722,20 @@ class Context:
         return out_packed, out_qp
 
     # -- cache of keys and values in 4 bits
-    def _kv_rows(self, x: torch.Tensor, cache: KVCache, batch: KVBatch, heads: int, what: str) -> tuple:
-        """(token stride, head stride) of a [tokens, heads, head_dim] tensor of this device."""
-        if not (x.device == self.device and x.dim() == 3 and x.shape[0] >= batch.tokens and x.shape[1] == heads
-                and x.shape[2] == cache.head_dim and x.stride(2) == 1):
-            raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} must be [tokens, {heads}, {cache.head_dim}] on {self.device}, the last "
-                                                     f"dimension contiguous, tokens at least {batch.tokens}")
-        return x.stride(0), x.stride(1)
+    def _kv_rows(self, x: torch.Tensor, tokens: int, heads: int, dim: int, what: str) -> tuple:
+        """(dtype code, token stride, head stride) of a [tokens, heads, head_dim] tensor of this device."""
+        got = _rows_of(x, self._index, tokens, heads, dim)
+        if got is None:
+            raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} must be [tokens, {heads}, {dim}] on {self.device}, the last dimension "
+                                                     f"contiguous, tokens at least {tokens}")
+        if got[0] < 0:
+            raise QuantPipeError(QP_ERR_UNSUPPORTED_DTYPE, f"unsupported dtype {x.dtype}")
+        return got
 
     def _kv_here(self, *parts) -> None:
         for p in parts:
-            t = p.pool if isinstance(p, KVCache) else p.pos if isinstance(p, KVBatch) else p
-            if t.device != self.device:
-                raise QuantPipeError(QP_ERR_INVALID_ARG, f"a cache, batch or list on {t.device}, the context on {self.device}")
+            if p._index != self._index:
+                raise QuantPipeError(QP_ERR_INVALID_ARG, f"a cache, batch or plan on cuda:{p._index}, the context on {self.device}")
 
     def qp_kv_extend(self, cache: KVCache, batch: KVBatch) -> torch.Tensor:
         """Pages for the batch's new tokens; fills and returns batch.pos and adds to cache.lens."""
@@ -742,11 +746,11 @@ class Context:
     def qp_kv_append(self, cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, layer: int = 0) -> None:
         """Quantizes the step's keys and values [tokens, heads, head_dim] into the cache's pages."""
         self._kv_here(cache, batch)
-        kt, kh = self._kv_rows(k, cache, batch, cache.heads, "k")
-        vt, vh = self._kv_rows(v, cache, batch, cache.heads, "v")
-        if k.dtype != v.dtype:
+        code, kt, kh = self._kv_rows(k, batch.tokens, cache.heads, cache.head_dim, "k")
+        v_code, vt, vh = self._kv_rows(v, batch.tokens, cache.heads, cache.head_dim, "v")
+        if code != v_code:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "k and v of different types")
-        self._run("qp_kv_append", cache._at, batch._at, layer, k, v, _dtype_code(k), kt, kh, vt, vh)
+        self._run("qp_kv_append", cache._at, batch._at, layer, k, v, code, kt, kh, vt, vh)
 
     def qp_kv_gather(self, cache: KVCache, batch: KVBatch, k: torch.Tensor | None = None, v: torch.Tensor | None = None,
                      layer: int = 0, out_dtype: torch.dtype = torch.float32):
@@ -754,11 +758,11 @@ class Context:
         self._kv_here(cache, batch)
         if k is None and v is None:
             k, v = torch.zeros(2, batch.tokens, cache.heads, cache.head_dim, dtype=out_dtype, device=self.device)
-        kt, kh = (0, 0) if k is None else self._kv_rows(k, cache, batch, cache.heads, "k")
-        vt, vh = (0, 0) if v is None else self._kv_rows(v, cache, batch, cache.heads, "v")
-        if k is not None and v is not None and k.dtype != v.dtype:
+        code, kt, kh = (None, 0, 0) if k is None else self._kv_rows(k, batch.tokens, cache.heads, cache.head_dim, "k")
+        v_code, vt, vh = (code, 0, 0) if v is None else self._kv_rows(v, batch.tokens, cache.heads, cache.head_dim, "v")
+        if code is not None and code != v_code:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "k and v of different types")
-        self._run("qp_kv_gather", cache._at, batch._at, layer, k, v, _dtype_code(v if k is None else k), kt, kh, vt, vh)
+        self._run("qp_kv_gather", cache._at, batch._at, layer, k, v, v_code, kt, kh, vt, vh)
         return k, v
 
     def qp_kv_attention_plan(self, cache: KVCache, q_heads: int, window: int = 0, scale: float | None = None) -> KVAttention:
@@ -770,41 +774,42 @@ class Context:
     def qp_kv_attention(self, cache: KVCache, batch: KVBatch, q: torch.Tensor, plan: KVAttention, layer: int = 0,
                         out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
         """Attention of q [tokens, q_heads, head_dim] over the cache; writes out (q's type) and, if given, lse [tokens, q_heads]."""
-        self._kv_here(cache, batch, plan.work)
-        qt, qh = self._kv_rows(q, cache, batch, plan.q_heads, "q")
+        self._kv_here(cache, batch, plan)
+        code, qt, qh = self._kv_rows(q, batch.tokens, plan.q_heads, cache.head_dim, "q")
         if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        ot, oh = self._kv_rows(out, cache, batch, plan.q_heads, "out")
-        if out.dtype != q.dtype:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out_code, ot, oh = self._kv_rows(out, batch.tokens, plan.q_heads, cache.head_dim, "out")
+        if out_code != code:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "out must have q's type")
-        if lse is not None and not (lse.dtype == torch.float32 and lse.device == self.device and lse.is_contiguous()
+        if lse is not None and not (lse.dtype == torch.float32 and lse.get_device() == self._index and lse.is_contiguous()
                                     and lse.numel() >= batch.tokens * plan.q_heads):
             raise QuantPipeError(QP_ERR_INVALID_ARG, "lse must be a contiguous float32 tensor [tokens, q_heads]")
-        self._run("qp_kv_attention", cache._at, batch._at, plan._at, layer, q, _dtype_code(q), qt, qh, out, ot, oh, lse)
+        self._run("qp_kv_attention", cache._at, batch._at, plan._at, layer, q, code, qt, qh, out, ot, oh, lse)
         return out
 
     def qp_kv_fork(self, cache: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:
         """Slots dst become copies of slots src: full pages shared, a part-filled one copied."""
         self._kv_here(cache)
-        _ints(src, "src", self.device), _ints(dst, "dst", self.device, src.numel())
-        self._run("qp_kv_fork", cache._at, src, dst, src.numel())
+        n = _ints(src, "src", self._index)
+        _ints(dst, "dst", self._index, n)
+        self._run("qp_kv_fork", cache._at, src, dst, n)
 
     def qp_kv_free(self, cache: KVCache, slots: torch.Tensor) -> None:
         self._kv_here(cache)
-        _ints(slots, "slots", self.device)
-        self._run("qp_kv_free", cache._at, slots, slots.numel())
+        self._run("qp_kv_free", cache._at, slots, _ints(slots, "slots", self._index))
 
     def qp_kv_copy_pages(self, cache: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:
         """Page dst[i] of every layer takes the bytes of page src[i]."""
         self._kv_here(cache)
-        _ints(src, "src", self.device), _ints(dst, "dst", self.device, src.numel())
-        self._run("qp_kv_copy_pages", cache._at, src, dst, src.numel())
+        n = _ints(src, "src", self._index)
+        _ints(dst, "dst", self._index, n)
+        self._run("qp_kv_copy_pages", cache._at, src, dst, n)
 
     def qp_kv_compact(self, cache: KVCache, live: torch.Tensor | None = None) -> None:
         """Moves the pages in use to the lowest numbers; live (one int32, or None) takes how many there are."""
         self._kv_here(cache)
         if live is not None:
-            _ints(live, "live", self.device, 1)
+            _ints(live, "live", self._index, 1)
         self._run("qp_kv_compact", cache._at, live)
 
     # -- host-buffer sender / receiver

@@ -15,7 +15,10 @@
  *   call64(number, *args)   the same for functions that return uint64
  *   tensor_in(x)            (numel, dtype code) of a contiguous CUDA tensor; AssertionError for others,
  *                           dtype code -1 for a dtype the library does not take
- *   setup(float32, bfloat16)  the two dtype objects that have a code; empties the table of bound functions
+ *   rows(x, device, tokens, heads, dim)  (dtype code, token stride, head stride) of a tensor [tokens or more, heads, dim] on
+ *                           that device, its last dimension contiguous; None for others (dtype code -1 as above)
+ *   ints(x, device)         elements of a contiguous int32 tensor on that device; -1 for others
+ *   setup(float32, bfloat16, int32)  the dtype objects that are known; empties the table of bound functions
  *
  * A tensor of one integer has an address and a value, so which of them is meant has to come from the parameter.
  * Every parameter of the functions called this way is an integer or a pointer, which the 64-bit C
@@ -29,7 +32,8 @@
 #define MAX_ARGS 16
 
 static PyObject *s_data_ptr, *s_numel, *s_is_contiguous, *s_is_cuda, *s_dtype;
-static PyObject *t_float32, *t_bfloat16;
+static PyObject *s_get_device, *s_shape, *s_stride;
+static PyObject *t_float32, *t_bfloat16, *t_int32;
 
 #define MAX_FUNCS 64
 static struct { uint64_t f; Py_ssize_t n; char kinds[MAX_ARGS + 1]; } funcs[MAX_FUNCS];
@@ -159,13 +163,79 @@ static PyObject* py_tensor_in(PyObject* m, PyObject* x)
     return r;
 }
 
+/* whether x lies on that device (a CPU tensor is on device -1); -1 on an error */
+static int is_on(PyObject* x, long device)
+{
+    PyObject* d = PyObject_CallMethodNoArgs(x, s_get_device);
+    if (!d) return -1;
+    const long at = PyLong_AsLong(d);
+    Py_DECREF(d);
+    return at == -1 && PyErr_Occurred() ? -1 : at == device && device >= 0;
+}
+
+static long long item_of(PyObject* tuple, Py_ssize_t i) { return PyLong_AsLongLong(PyTuple_GET_ITEM(tuple, i)); }
+
+static PyObject* py_rows(PyObject* m, PyObject* const* args, Py_ssize_t n)
+{
+    (void)m;
+    if (n != 5) { PyErr_SetString(PyExc_TypeError, "rows(x, device, tokens, heads, dim)"); return NULL; }
+    PyObject* x = args[0];
+    const long device = PyLong_AsLong(args[1]);
+    const long long tokens = PyLong_AsLongLong(args[2]), heads = PyLong_AsLongLong(args[3]), dim = PyLong_AsLongLong(args[4]);
+    if (PyErr_Occurred()) return NULL;
+    const int here = is_on(x, device);
+    if (here < 0) return NULL;
+    if (!here) Py_RETURN_NONE;
+    PyObject* shape = PyObject_GetAttr(x, s_shape);
+    if (!shape) return NULL;
+    const int fits = PyTuple_Check(shape) && PyTuple_GET_SIZE(shape) == 3 && item_of(shape, 0) >= tokens &&
+                     item_of(shape, 1) == heads && item_of(shape, 2) == dim;
+    Py_DECREF(shape);
+    if (PyErr_Occurred()) return NULL;
+    if (!fits) Py_RETURN_NONE;
+    PyObject* stride = PyObject_CallMethodNoArgs(x, s_stride);
+    if (!stride) return NULL;
+    if (!PyTuple_Check(stride) || PyTuple_GET_SIZE(stride) != 3) { Py_DECREF(stride); Py_RETURN_NONE; }
+    const long long st = item_of(stride, 0), sh = item_of(stride, 1), sd = item_of(stride, 2);
+    Py_DECREF(stride);
+    if (PyErr_Occurred()) return NULL;
+    if (sd != 1) Py_RETURN_NONE;
+    PyObject* dtype = PyObject_GetAttr(x, s_dtype);
+    if (!dtype) return NULL;
+    const int code = dtype == t_float32 ? 0 : dtype == t_bfloat16 ? 1 : -1;
+    Py_DECREF(dtype);
+    return Py_BuildValue("iLL", code, st, sh);
+}
+
+static PyObject* py_ints(PyObject* m, PyObject* const* args, Py_ssize_t n)
+{
+    (void)m;
+    if (n != 2) { PyErr_SetString(PyExc_TypeError, "ints(x, device)"); return NULL; }
+    PyObject* x = args[0];
+    const long device = PyLong_AsLong(args[1]);
+    if (PyErr_Occurred()) return NULL;
+    const int here = is_on(x, device);
+    if (here < 0) return NULL;
+    if (!here) return PyLong_FromLong(-1);
+    PyObject* dtype = PyObject_GetAttr(x, s_dtype);
+    if (!dtype) return NULL;
+    const int whole = dtype == t_int32;
+    Py_DECREF(dtype);
+    if (!whole) return PyLong_FromLong(-1);
+    const int contiguous = is_true(PyObject_CallMethodNoArgs(x, s_is_contiguous));
+    if (contiguous < 0) return NULL;
+    return contiguous ? PyObject_CallMethodNoArgs(x, s_numel) : PyLong_FromLong(-1);
+}
+
 static PyObject* py_setup(PyObject* m, PyObject* args)
 {
-    PyObject *f, *b;
+    PyObject *f, *b, *i;
     (void)m;
-    if (!PyArg_ParseTuple(args, "OO", &f, &b)) return NULL;
+    if (!PyArg_ParseTuple(args, "OOO", &f, &b, &i)) return NULL;
     Py_INCREF(f);
     Py_INCREF(b);
+    Py_INCREF(i);
+    Py_XSETREF(t_int32, i);
     Py_XSETREF(t_float32, f);
     Py_XSETREF(t_bfloat16, b);
     n_funcs = 0;
@@ -177,7 +247,9 @@ static PyMethodDef methods[] = {
     {"call", (PyCFunction)(void (*)(void))py_call, METH_FASTCALL, "call(number, *args) -> int32 status"},
     {"call64", (PyCFunction)(void (*)(void))py_call64, METH_FASTCALL, "call64(number, *args) -> uint64"},
     {"tensor_in", py_tensor_in, METH_O, "tensor_in(x) -> (numel, dtype code)"},
-    {"setup", py_setup, METH_VARARGS, "setup(float32, bfloat16)"},
+    {"rows", (PyCFunction)(void (*)(void))py_rows, METH_FASTCALL, "rows(x, device, tokens, heads, dim) -> (dtype code, strides)"},
+    {"ints", (PyCFunction)(void (*)(void))py_ints, METH_FASTCALL, "ints(x, device) -> elements"},
+    {"setup", py_setup, METH_VARARGS, "setup(float32, bfloat16, int32)"},
     {NULL, NULL, 0, NULL},
 };
 
@@ -191,6 +263,10 @@ PyMODINIT_FUNC PyInit__qpcall(void)
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_is_cuda = PyUnicode_InternFromString("is_cuda");
     s_dtype = PyUnicode_InternFromString("dtype");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
+    if (!s_get_device || !s_shape || !s_stride) return NULL;
     if (!s_data_ptr || !s_numel || !s_is_contiguous || !s_is_cuda || !s_dtype) return NULL;
     return PyModule_Create(&module);
 }
