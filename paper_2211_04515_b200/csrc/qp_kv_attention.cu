@@ -40,6 +40,7 @@ constexpr float M_SLACK = 8.f;                   // a score may pass the referen
 constexpr float V_SLACK = 64.f;                  // and a scale of V its norm by this: p * scale' <= 2^14 in fp16
 constexpr int UNIT = 4;                          // slices
 constexpr int HEAD = 3;                          // units
+constexpr int MANY = 64;                         // query rows to a cached head from which on the tensor-memory kernel is the faster
 
 template <int D, int NT, bool SPLIT> struct Cfg {
     static constexpr int ROWS = 8 * NT;
@@ -150,7 +151,7 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
     const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
     q.n = row1 - q.row0;
     if (q.n > a.max_new) q.n = a.max_new;
-    if (q.n <= 0 || q.pos < 0) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return q; }
+    if (q.n <= 0 || q.pos < 0 || (int64_t)q.n * a.group >= a.many) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return q; }
     const int64_t most = (int64_t)a.pages.max_pages * a.pages.page_size;
     int64_t end = (int64_t)q.pos + q.n;
     if (end > most) end = most;
@@ -793,7 +794,8 @@ extern "C" uint64_t qp_kv_attention_work_bytes(qp_ctx* ctx, const qp_kv_cache_t*
 {
     if (!ctx || !h_cache || !qp_kv_dim_ok(h_cache->head_dim)) return 0;
     const uint64_t blocks = (uint64_t)ctx->sm_count * MAX_PER_SM;
-    return QP_KV_COUNTERS * 4 + blocks * 2 * MAX_ROWS * (uint64_t)(h_cache->head_dim + 2) * 4;
+    const uint64_t few = blocks * 2 * MAX_ROWS * (uint64_t)(h_cache->head_dim + 2) * 4, many = qp_kv_chunk_part_bytes(h_cache->head_dim, ctx->sm_count);
+    return QP_KV_COUNTERS * 4 + (few > many ? few : many);
 }
 
 extern "C" int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batch_t* h_batch, const qp_kv_attention_t* h_plan,
@@ -841,7 +843,15 @@ extern "C" int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, co
     a.count = static_cast<unsigned*>(h_plan->d_work);
     a.part = reinterpret_cast<float*>(a.count + QP_KV_COUNTERS);
     a.status = ctx->d_status;
-    const Launch f = choose(c->head_dim, dtype == QP_F32, (int64_t)a.max_new * group);
+    a.many = 0x7FFFFFFF;
+    a.wait_cycles = ctx->wait_cycles;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (dtype == QP_BF16 && c->head_dim <= 128 && (int64_t)a.max_new * group >= MANY) {
+        a.many = MANY;
+        rc = qp_kv_chunk_launch(ctx, a, c->head_dim, s);
+        if (rc) return rc;
+    }
+    const Launch f = choose(c->head_dim, dtype == QP_F32, a.many < 0x7FFFFFFF ? a.many - 1 : (int64_t)a.max_new * group);
     const int grid = ctx->sm_count * f.per_sm;
     if (2 * grid > QP_KV_COUNTERS / 2) return qp_fail(ctx, QP_ERR_INVALID_ARG, "device with more SMs than the workspace has counters for");
     if (ctx->device >= QP_KV_MAX_DEVICES || !f.ready[ctx->device]) {
@@ -850,7 +860,7 @@ extern "C" int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, co
         if (ctx->device < QP_KV_MAX_DEVICES) f.ready[ctx->device] = true;
     }
     void* args[] = {&a};
-    cudaLaunchKernel(f.kernel, dim3((unsigned)grid), dim3(THREADS), args, (size_t)f.smem, static_cast<cudaStream_t>(stream));
+    cudaLaunchKernel(f.kernel, dim3((unsigned)grid), dim3(THREADS), args, (size_t)f.smem, s);
     ctx->launches += 1;
     return qp_check_launch(ctx, "qp_kv_attention");
 }

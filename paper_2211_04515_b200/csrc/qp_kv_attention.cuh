@@ -24,4 +24,10 @@ struct qp_kv_attn_args {
     unsigned* count;
     float* part;
     unsigned* status;
+    int many;                                    // sequences with so many query rows to a cached head, or more, are qp_kv_chunk.cu's
+    long long wait_cycles;
 };
+
+// qp_kv_chunk.cu: the sequences with many rows.  Workspace for parts of items, and the launch.
+uint64_t qp_kv_chunk_part_bytes(int head_dim, int sm_count);
+int32_t qp_kv_chunk_launch(qp_ctx* ctx, const qp_kv_attn_args& a, int head_dim, cudaStream_t s);

@@ -1,0 +1,781 @@
+// Attention over the 4-bit cache for many queries to a cached head (chunks of a prompt), bf16, on tcgen05.
+//
+// An item is 256 query rows of one cached head (row = token * group + query head of the group: all of them read the same
+// keys) as two tiles of 128, against the keys they see in tiles of 128.  Per key tile and query tile
+//     S = Q K^T    128 x 128 x D, both operands in shared memory, S in tensor memory
+//     P = 2^(S f - m)   a thread to a row
+//     O += P V     P from tensor memory (over S), V in shared memory, O in tensor memory
+//
+// Roles: warps 0-3 and 4-7 are the rows of query tiles 0 and 1; warps 8-11 turn the cache's codes into fp16 operands; one
+// thread of warp 12 issues the products.  The two query tiles take turns: one's softmax runs while the other's products do.
+//
+// What bounds it: 4 * 256 * 128 * D operations of the products (2048 cycles at D = 128 and the nominal rate) and as many cycles for
+// the 32768 exponentials (16 a cycle).  So a softmax element gets three more operations and no more: the codes are not multiplied
+// as they are, as for few queries (their quantizers would cost two operations and shared-memory reads on every score and weight), but
+// as lo + scale * code, put together in fp32 and rounded once to fp16.  That costs 20 operations to 8 codes, a third of
+// the softmax's for 256 rows.  The rounding is 2^-11 of a value at most, an eighth of what the rounding of K to bf16 would be.  fp16's
+// range: each tile of K and of V is scaled by a power of two that takes its largest value to [2^10, 2^11); queries are scaled by
+// row.  K's power goes into the factor of the scores, V's into the exponent of the weights (both are one number a tile).
+//
+//   - Softmax reference raised only when a score passes it by 8 (log2): then O is read from tensor memory, scaled and put back.
+//   - The work, in key tiles, is cut into equal runs for the SMs; an item that a cut falls into leaves partial results
+//     and the last block to finish adds them (as for few queries).
+//   - Every wait has a limit: a block that gives up raises QP_DEV_STREAM_TIMEOUT, its roles leave, the products in flight are
+//     waited for, tensor memory is freed.
+#include "qp_kv.cuh"
+#include "qp_kv_attention.cuh"
+#include "qp_stream.cuh"
+
+QP_CK_UNIT
+
+namespace {
+
+constexpr int THREADS = 512, TILE = 128, ROWS = 2 * TILE;
+constexpr int HEAD = 2;                          // what an item costs beside its key tiles, in key tiles
+constexpr int MIN_RUN = 4;                       // key tiles that are worth a block
+constexpr int SEGS = 32;                         // parts of items that are listed at a time
+constexpr float M_NONE = -3.0e38f, M_SLACK = 8.f;
+constexpr int P_SHIFT = 5;                       // weights are 2^5 higher: up to 2^13 in fp16
+
+template <int D> struct Cfg {
+    static constexpr int OPERAND = TILE * D * 2;                 // bytes of Q, K, V tiles
+    static constexpr int SMEM = 1024 + 6 * OPERAND;
+    static constexpr int PART = TILE * (D + 2);                  // floats of a query tile's partial result
+    static constexpr int SB = qp_kv_slice<D>::BYTES;
+    static constexpr int LOADS = TILE * (D / 2) / 16 / 128;      // 16-byte loads of a thread for K's codes of a tile
+};
+
+// ---------------------------------------------------------------------------- tcgen05
+
+__device__ __forceinline__ uint32_t smem_of(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+// operand in shared memory: rows of 128 bytes, 16-byte pieces exchanged within 8 rows (128-byte swizzle).  K-major: the row is the
+// M or N index, eight rows 1024 bytes on; MN-major: the row is the K index, 64 elements of M or N to a panel, panels `lead` bytes apart
+__device__ __forceinline__ uint64_t operand_at(uint32_t addr, uint32_t lead)
+{
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (uint64_t)(lead >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+// fp16 x fp16 -> fp32, M = 128
+__host__ __device__ constexpr uint32_t shape_of(int n, bool b_mn_major)
+{
+    return 1u << 4 | (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (uint32_t)(128 / 16) << 24;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
+{
+    asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d), "l"(a), "l"(b),
+                 "r"(shape), "r"((uint32_t)add)
+                 : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add)
+{
+    asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d), "r"(a), "l"(b),
+                 "r"(shape), "r"((uint32_t)add)
+                 : "memory");
+}
+__device__ __forceinline__ void commit(uint64_t* bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_of(bar)) : "memory");
+}
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+// the loads into x are there: nothing that uses x may move in front of this
+template <int N>
+__device__ __forceinline__ void wait_ld(float (&x)[N])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(x[i]));
+}
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void fence_operands() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// 32 columns of a warp's 32 rows, a row to a lane
+__device__ __forceinline__ void tmem_ld32(uint32_t at, float* x)
+{
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,"
+        "%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(at));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const float* x)
+{
+    const uint32_t* r = reinterpret_cast<const uint32_t*>(x);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,"
+        "%26,%27,%28,%29,%30,%31,%32};" ::"r"(at),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+        "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]),
+        "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t* r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(at), "r"(r[0]),
+                 "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]),
+                 "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ unsigned half2_of(float lo, float hi)
+{
+    unsigned r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ unsigned half2_of(qp_f2 v)
+{
+    float a, b;
+    qp_unpack2(v, a, b);
+    return half2_of(a, b);
+}
+__device__ __forceinline__ void arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_of(bar)) : "memory"); }
+template <int ID> __device__ __forceinline__ void group_sync() { asm volatile("bar.sync %0, 128;" ::"n"(ID) : "memory"); }
+__device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e < -126 ? 1 : e > 127 ? 254 : e + 127) << 23); }
+
+// ---------------------------------------------------------------------------- work
+
+// a part of an item: key tiles [u0, u1) of query rows tile * ROWS ..
+struct Seg {
+    int pos, n, row0, slot, head, tile, u0, u1;
+    int s0;                                      // slice that key tile 0 begins with
+    int split, c0, c1, first_at, at;             // parts of the item: blocks c0 .. c1, places of the first and of this one
+};
+
+struct Shared {
+    uint64_t q_full[2], kv_full[2], kv_empty[2], s_full[2], p_full[2], pv_done[2], all_done;
+    uint32_t tmem, give_up;
+    int n_segs, more;
+    float kinv[2];                               // per stage: what takes K's scaled values back
+    int ve[2];                                   // the power of two that V's were divided by
+    uint32_t valid[2][4];                        // keys that are there
+    float2 quant[2][2][TILE];                    // K's and V's quantizers of a tile
+    float amax[2][2][4];
+    int last[2];
+    Seg segs[SEGS];
+};
+
+struct Seq { int pos, n, row0, slot, tiles; };
+
+__device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
+{
+    Seq q;
+    q.pos = __ldg(a.rows.pos + b);
+    q.slot = qp_kv_slot(a.rows, b);
+    q.row0 = qp_kv_start(a.rows, b);
+    const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
+    q.n = row1 - q.row0;
+    if (q.n > a.max_new) q.n = a.max_new;
+    const int64_t rows = (int64_t)q.n * a.group;
+    q.tiles = q.n <= 0 || q.pos < 0 || rows < a.many ? 0 : (int)((rows + ROWS - 1) / ROWS);
+    return q;
+}
+// slices [first, first + 8 * returned) hold the keys that rows tile * ROWS .. see
+__device__ __forceinline__ int tiles_of(const qp_kv_attn_args& a, const Seq& q, int tile, int& first)
+{
+    const int64_t most = (int64_t)a.pages.max_pages * a.pages.page_size;
+    const int64_t r0 = (int64_t)tile * ROWS, all = (int64_t)q.n * a.group, r1 = r0 + ROWS < all ? r0 + ROWS : all;
+    int64_t end = (int64_t)q.pos + (r1 - 1) / a.group + 1, lo = a.window > 0 ? (int64_t)q.pos + r0 / a.group - a.window + 1 : 0;
+    if (end > most) end = most;
+    if (lo < 0) lo = 0;
+    if (lo > end) lo = end;
+    first = (int)(lo / QP_KV_SLICE);
+    const int64_t slices = (end + QP_KV_SLICE - 1) / QP_KV_SLICE - first;
+    return slices < 1 ? 1 : (int)((slices + TILE / QP_KV_SLICE - 1) / (TILE / QP_KV_SLICE));
+}
+__device__ __forceinline__ int64_t work_of(const qp_kv_attn_args& a, const Seq& q)      // of one head
+{
+    int64_t w = 0;
+    int first;
+    for (int t = 0; t < q.tiles; ++t) w += HEAD + tiles_of(a, q, t, first);
+    return w;
+}
+
+// lists the block's next parts, from unit u on; warp 0.  b: the sequence, base: work in front of it
+__device__ __forceinline__ void list_parts(const qp_kv_attn_args& a, Shared& sh, int64_t& u, int64_t end, int64_t begin, int64_t W,
+                                           int64_t blocks, int& b, int64_t& base)
+{
+    int n = 0;
+    while (u < end && n < SEGS) {
+        Seq q = seq_of(a, b);
+        int64_t one = work_of(a, q);
+        while (u >= base + one * a.heads) {
+            base += one * a.heads;
+            q = seq_of(a, ++b);
+            one = work_of(a, q);
+        }
+        int head = (int)((u - base) / one);
+        int64_t i0 = base + head * one;
+        while (u < end && head < a.heads && n < SEGS) {
+            int tile = 0, first, units = HEAD + tiles_of(a, q, 0, first);
+            while (u >= i0 + units) { i0 += units; units = HEAD + tiles_of(a, q, ++tile, first); }
+            for (; tile < q.tiles && u < end && n < SEGS; ++tile) {
+                units = HEAD + tiles_of(a, q, tile, first);
+                const int g0 = (int)(u - i0), g1 = units - g0 < end - u ? units : g0 + (int)(end - u);
+                const int u0 = g0 > HEAD ? g0 - HEAD : 0, u1 = g1 - HEAD;
+                if (u1 > u0) {
+                    Seg s;
+                    s.pos = q.pos; s.n = q.n; s.row0 = q.row0; s.slot = q.slot; s.head = head; s.tile = tile;
+                    s.u0 = u0; s.u1 = u1; s.s0 = first;
+                    s.split = u0 > 0 || u1 < units - HEAD;
+                    s.c0 = s.c1 = s.first_at = s.at = 0;
+                    if (s.split) {
+                        s.c0 = (int)(((i0 + HEAD + 1) * blocks - 1) / W);
+                        s.c1 = (int)(((i0 + units) * blocks - 1) / W);
+                        s.first_at = 2 * s.c0 + ((int64_t)s.c0 * W / blocks < i0 ? 1 : 0);
+                        s.at = 2 * (int)blockIdx.x + (u == begin ? 0 : 1);
+                    }
+                    if ((threadIdx.x & 31) == 0) sh.segs[n] = s;
+                    ++n;
+                }
+                u += g1 - g0;
+                i0 += units;
+            }
+            ++head;
+        }
+    }
+    if ((threadIdx.x & 31) == 0) { sh.n_segs = n; sh.more = u < end; }
+}
+
+// A wait with a limit.  Once one has run out none waits any more: every role goes on to the end of its loops, so that no barrier is
+// left with a part of its threads, and nothing more is written out.
+__device__ __forceinline__ bool given_up(const Shared& sh) { return *(const volatile uint32_t*)&sh.give_up != 0u; }
+__device__ __forceinline__ void wait(Shared& sh, uint64_t* bar, unsigned parity, long long limit)
+{
+    if (qp_stream::mbar_try_wait(bar, parity)) return;
+    const long long since = clock64();
+    while (!qp_stream::mbar_try_wait(bar, parity)) {
+        if (given_up(sh)) return;
+        if (clock64() - since > limit) {
+            *(volatile uint32_t*)&sh.give_up = 1u;
+            return;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------- the cache's codes into operands
+
+template <int D>
+__device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, char* stages, int& g)
+{
+    using C = Cfg<D>;
+    using S = qp_kv_slice<D>;
+    constexpr int L = C::LOADS, PER = 16 * (D / 32);             // 16-byte pieces of a slice's K (or V) codes
+    const int p = threadIdx.x & 127, lane = p & 31;
+    // this thread's piece of a slice: row and 32 elements; eight lanes take eight rows, so that their stores meet all banks
+    const int in = p & (PER - 1), row = (in & 7) + 8 * ((in >> 3) & (D == 128 ? 0 : 1)) + (D == 128 ? 8 * (in >> 5) : 0);
+    const int piece = D == 128 ? (in >> 3) & 3 : in >> 4;
+    for (int i = 0; i < sh.n_segs; ++i) {
+        const Seg& s = sh.segs[i];
+        const int held = s.pos + s.n, units = s.u1 - s.u0;
+        uint4 k[L], v[L];
+        float4 quant;
+        // what the tile needs from memory, into registers
+        auto load = [&](int u) {
+            const int first = s.s0 + 8 * u;
+            int64_t place = -1;
+            if (lane < 8) {                                      // lane i of each warp: slice i
+                const int sl = first + lane, pg = sl / a.slices;
+                const int64_t at = (int64_t)sl * QP_KV_SLICE;
+                if (at < held) {
+                    const int page = qp_kv_page(a.pages, s.slot, pg * a.pages.page_size);
+                    if (page >= 0) place = (((int64_t)page * a.heads + s.head) * a.slices + (sl - pg * a.slices)) * C::SB;
+                    else atomicOr(a.status, QP_DEV_KV_RANGE);
+                }
+            }
+#pragma unroll
+            for (int l = 0; l < L; ++l) {
+                const int sl = (l * 128 + p) / PER;
+                const int64_t at = __shfl_sync(0xFFFFFFFFu, place, sl);
+                const char* x = a.pool + at + row * S::ROW + piece * 16;
+                k[l] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(x)) : make_uint4(0, 0, 0, 0);
+                v[l] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(x + S::V)) : make_uint4(0, 0, 0, 0);
+            }
+            const int64_t mine = __shfl_sync(0xFFFFFFFFu, place, p / QP_KV_SLICE);
+            quant = make_float4(0.f, 0.f, 0.f, 0.f);
+            const bool there = mine >= 0 && first * QP_KV_SLICE + p < held;
+            if (there) {
+                const float2 kq = __ldg(reinterpret_cast<const float2*>(a.pool + mine + S::KQ + p % QP_KV_SLICE * 8));
+                const float2 vq = __ldg(reinterpret_cast<const float2*>(a.pool + mine + S::VQ + p % QP_KV_SLICE * 8));
+                quant = make_float4(kq.x, kq.y, vq.x, vq.y);
+            }
+            return __ballot_sync(0xFFFFFFFFu, there);
+        };
+        unsigned there = load(s.u0);
+        for (int u = 0; u < units; ++u, ++g) {
+            const int st = g & 1;
+            // powers of two for the tile
+            float ka = fmaxf(fabsf(quant.x), fabsf(fmaf(15.f, quant.y, quant.x))), va = fmaxf(fabsf(quant.z), fabsf(fmaf(15.f, quant.w, quant.z)));
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                ka = fmaxf(ka, __shfl_xor_sync(0xFFFFFFFFu, ka, o));
+                va = fmaxf(va, __shfl_xor_sync(0xFFFFFFFFu, va, o));
+            }
+            if (lane == 0) { sh.amax[st][0][p >> 5] = ka; sh.amax[st][1][p >> 5] = va; }
+            sh.quant[st][0][p] = make_float2(quant.x, quant.y);
+            sh.quant[st][1][p] = make_float2(quant.z, quant.w);
+            group_sync<1>();
+#pragma unroll
+            for (int w = 0; w < 4; ++w) { ka = fmaxf(ka, sh.amax[st][0][w]); va = fmaxf(va, sh.amax[st][1][w]); }
+            int ke = (int)(__float_as_uint(ka) >> 23) - 127 - 10, ve = (int)(__float_as_uint(va) >> 23) - 127 - 10;
+            ke = ke < -100 ? -100 : ke;                          // (all but zero: nothing to gain)
+            ve = ve < -100 ? -100 : ve;
+            const float kf = pow2(-ke), vf = pow2(-ve);
+            if (g >= 2) wait(sh, &sh.kv_empty[st], ((g >> 1) + 1) & 1, a.wait_cycles);
+            __syncwarp();
+            char* to = stages + st * (2 * C::OPERAND);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float f = h ? vf : kf;
+#pragma unroll
+                for (int l = 0; l < L; ++l) {
+                    const int sl = (l * 128 + p) / PER, key = sl * QP_KV_SLICE + row;
+                    const float2 q = sh.quant[st][h][key];
+                    // a nibble under 128's (or 2048's) exponent is 128 + code: lo + scale * code in one fused operation
+                    const float sc = q.y * f, lo = q.x * f;
+                    const qp_f2 s2 = qp_pack2(sc, sc), c2 = qp_pack2(fmaf(-128.f, sc, lo), fmaf(-2048.f, sc, lo));
+                    const uint4 raw = h ? v[l] : k[l];
+                    const unsigned w4[4] = {raw.x, raw.y, raw.z, raw.w};
+                    char* panel = to + h * C::OPERAND + (D == 128 ? (piece >> 1) * (TILE * 128) : 0) + key * 128;
+                    const int c0 = D == 128 ? 4 * (piece & 1) : 4 * piece;
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const unsigned x[4] = {w4[w] << 16, w4[w] << 8, w4[w], w4[w] >> 8};   // bits 16..19: codes 0, 2, 4, 6
+                        const unsigned y[4] = {w4[w] << 8, w4[w], w4[w] >> 8, w4[w] >> 16};   // bits 12..15: codes 1, 3, 5, 7
+                        uint4 out;
+                        unsigned* o = &out.x;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            o[e] = half2_of(qp_fma2(qp_pack2(__uint_as_float((x[e] & 0x000F0000u) | 0x43000000u),
+                                                             __uint_as_float((y[e] & 0x0000F000u) | 0x45000000u)), s2, c2));
+                        *reinterpret_cast<uint4*>(panel + (((c0 + w) ^ (key & 7)) << 4)) = out;
+                    }
+                }
+            }
+            if (p == 0) { sh.kinv[st] = pow2(ke); sh.ve[st] = ve; }
+            if (lane == 0) sh.valid[st][p >> 5] = there;
+            fence_operands();
+            arrive(&sh.kv_full[st]);
+            if (u + 1 < units) there = load(s.u0 + u + 1);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------- products
+
+template <int D>
+__device__ __forceinline__ void multiply(const qp_kv_attn_args& a, Shared& sh, char* q_at, char* stages, int& g, int& items)
+{
+    using C = Cfg<D>;
+    constexpr uint32_t S_SHAPE = shape_of(TILE, false), O_SHAPE = shape_of(D, true);
+    const uint32_t q0 = smem_of(q_at), kv0 = smem_of(stages), tm = sh.tmem;
+    auto scores = [&](int t, int st) {
+#pragma unroll
+        for (int s = 0; s < D / 16; ++s) {
+            const uint32_t in = (uint32_t)(s >> 2) * (TILE * 128) + (uint32_t)(s & 3) * 32;
+            mma_ss(tm + t * TILE, operand_at(q0 + t * C::OPERAND + in, 16), operand_at(kv0 + st * 2 * C::OPERAND + in, 16), S_SHAPE, s > 0);
+        }
+        commit(&sh.s_full[t]);
+    };
+    for (int i = 0; i < sh.n_segs; ++i, ++items) {
+        const int units = sh.segs[i].u1 - sh.segs[i].u0;
+        wait(sh, &sh.kv_full[g & 1], (g >> 1) & 1, a.wait_cycles);
+        for (int t = 0; t < 2; ++t) {
+            wait(sh, &sh.q_full[t], items & 1, a.wait_cycles);
+            fence_after();
+            scores(t, g & 1);
+        }
+        for (int u = 0; u < units; ++u, ++g) {
+            const int st = g & 1;
+            for (int t = 0; t < 2; ++t) {
+                wait(sh, &sh.p_full[t], g & 1, a.wait_cycles);
+                fence_after();
+#pragma unroll
+                for (int s = 0; s < TILE / 16; ++s)
+                    mma_ts(tm + 2 * TILE + t * TILE, tm + t * TILE + s * 8, operand_at(kv0 + (st * 2 + 1) * C::OPERAND + s * 2048, TILE * 128), O_SHAPE,
+                           u > 0 || s > 0);
+                commit(&sh.pv_done[t]);
+                if (t == 1) commit(&sh.kv_empty[st]);
+                if (u + 1 < units) {                             // the next scores take the place of the weights just used
+                    if (t == 0) wait(sh, &sh.kv_full[st ^ 1], ((g + 1) >> 1) & 1, a.wait_cycles);
+                    wait(sh, &sh.pv_done[t], g & 1, a.wait_cycles);
+                    fence_after();
+                    scores(t, st ^ 1);
+                }
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------- softmax
+
+// this row's out and lse
+template <int D>
+__device__ __forceinline__ void put_row(const qp_kv_attn_args& a, const Seg& s, int64_t r, int d, float4 o, float m, float l, bool bad)
+{
+    const int64_t token = s.row0 + r / a.group;
+    const int h = s.head * a.group + (int)(r % a.group);
+    const float nan = __int_as_float(0x7FC00000);
+    float v[4] = {o.x, o.y, o.z, o.w};
+    unsigned short x[4];
+    unsigned short* to = static_cast<unsigned short*>(a.out) + token * a.ot + (int64_t)h * a.oh + d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = qp_f32_to_bf16(bad ? nan : l == 0.f ? 0.f : v[i] / l);
+    if (a.out_vec) *reinterpret_cast<uint2*>(to) = make_uint2(x[0] | ((unsigned)x[1] << 16), x[2] | ((unsigned)x[3] << 16));
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = x[i];
+    if (a.lse && d == 0) a.lse[token * a.q_heads + h] = bad ? nan : l == 0.f ? -__int_as_float(0x7F800000) : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+template <int D>
+__device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, char* q_at, int& g)
+{
+    using C = Cfg<D>;
+    const int t = threadIdx.x >> 7, row = threadIdx.x & 127, lane = threadIdx.x & 31;
+    const uint32_t lanes = (uint32_t)(row & ~31) << 16;
+    const uint32_t s_at = sh.tmem + t * TILE + lanes, o_at = sh.tmem + 2 * TILE + t * TILE + lanes;
+    const float inf = __int_as_float(0x7F800000);
+    for (int i = 0; i < sh.n_segs; ++i) {
+        const Seg& s = sh.segs[i];
+        const int64_t r = (int64_t)s.tile * ROWS + t * TILE + row, all = (int64_t)s.n * a.group;
+        const bool mine = r < all;
+        // ---- the query row, scaled, into shared memory
+        float kf;
+        bool bad;
+        {
+            uint4 x[D / 8];
+            const unsigned short* from = static_cast<const unsigned short*>(a.q);
+            if (mine) from += (s.row0 + r / a.group) * a.qt + (int64_t)(s.head * a.group + (int)(r % a.group)) * a.qh;
+            if (!mine) {
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) x[c] = make_uint4(0, 0, 0, 0);
+            } else if (a.vec) {
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) x[c] = __ldg(reinterpret_cast<const uint4*>(from) + c);
+            } else {
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    unsigned w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = __ldg(from + 8 * c + 2 * e) | ((unsigned)__ldg(from + 8 * c + 2 * e + 1) << 16);
+                    x[c] = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+            float top = 0.f;
+            bool nan = false;
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+                const unsigned w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float y0 = fabsf(__uint_as_float(w[e] << 16)), y1 = fabsf(__uint_as_float(w[e] & 0xFFFF0000u));
+                    nan |= !(y0 < inf) || !(y1 < inf);
+                    top = qp_max3(top, y0, y1);
+                }
+            }
+            bad = nan;
+            int ex = 265 - (int)(__float_as_uint(top) >> 23);    // the row's largest element to [2^11, 2^12)
+            ex = top == 0.f || bad ? 127 : ex > 254 ? 254 : ex;
+            float norm = __uint_as_float((unsigned)ex << 23);
+            kf = fabsf(a.scale_log2) / norm;
+            norm = bad ? 0.f : a.scale_log2 < 0.f ? -norm : norm;
+            char* to = q_at + t * C::OPERAND + row * 128;
+#pragma unroll
+            for (int c = 0; c < D / 8; ++c) {
+                const unsigned w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+                unsigned h[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float y0 = __uint_as_float(w[e] << 16), y1 = __uint_as_float(w[e] & 0xFFFF0000u);
+                    h[e] = bad ? 0u : half2_of(y0 * norm, y1 * norm);
+                }
+                *reinterpret_cast<uint4*>(to + (c >> 3) * (TILE * 128) + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
+            }
+            fence_operands();
+            arrive(&sh.q_full[t]);
+        }
+        // last key that the row sees; keys in front of all_hi and from all_lo on are seen by every row of the tile
+        const int64_t last_row = (int64_t)s.tile * ROWS + t * TILE + TILE < all ? (int64_t)s.tile * ROWS + t * TILE + TILE - 1 : all - 1;
+        const int64_t hi = s.pos + (mine ? r : all - 1) / a.group;
+        const int64_t all_hi = s.pos + ((int64_t)s.tile * ROWS + t * TILE) / a.group + 1;
+        const int64_t all_lo = a.window > 0 ? s.pos + last_row / a.group - a.window + 1 : 0;
+        float m = M_NONE, l = 0.f;
+        int E = -1000;                                           // O holds sums of p * v * 2^(P_SHIFT - E)
+        for (int u = s.u0; u < s.u1; ++u, ++g) {
+            const int st = g & 1;
+            const int64_t t0 = ((int64_t)s.s0 + 8 * u) * QP_KV_SLICE;
+            wait(sh, &sh.kv_full[st], (g >> 1) & 1, a.wait_cycles);      // (long there: for what the producers say of the tile)
+            wait(sh, &sh.s_full[t], g & 1, a.wait_cycles);
+            __syncwarp();
+            fence_after();
+            float x[TILE];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, x + 32 * c);
+            const float f = fmaxf(kf * sh.kinv[st], 1e-37f);     // (positive, so that -inf stays)
+            const int ve = sh.ve[st];
+            wait_ld(x);
+            const unsigned valid = sh.valid[st][0] & sh.valid[st][1] & sh.valid[st][2] & sh.valid[st][3];
+            if (valid != 0xFFFFFFFFu || t0 < all_lo || t0 + TILE > all_hi) {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int64_t up = hi - t0 - 32 * c, down = a.window > 0 ? hi - a.window - t0 - 32 * c : -1;   // keys (down, up]
+                    unsigned seen = sh.valid[st][c];
+                    seen &= up < 0 ? 0u : up >= 31 ? 0xFFFFFFFFu : (2u << up) - 1u;
+                    seen &= down < 0 ? 0xFFFFFFFFu : down >= 31 ? 0u : ~((2u << down) - 1u);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) x[32 * c + e] = seen >> e & 1u ? x[32 * c + e] : -inf;
+                }
+            }
+            float top4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+            for (int c = 4; c < TILE; c += 8)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top4[e] = c + 4 + e < TILE ? qp_max3(top4[e], x[c + e], x[c + 4 + e]) : fmaxf(top4[e], x[c + e]);
+            const float top = fmaxf(qp_max3(top4[0], top4[1], top4[2]), top4[3]) * f;
+            if (__any_sync(0xFFFFFFFFu, top > m + M_SLACK || ve > E)) {     // rare: a new reference
+                const float next = fmaxf(m, top);
+                float back = ex2(m - next);
+                m = next;
+                l *= back;
+                if (ve > E) {
+                    back *= E < -999 ? 0.f : pow2(E - ve);
+                    E = ve;
+                }
+                if (u > s.u0) {
+                    wait(sh, &sh.pv_done[t], (g - 1) & 1, a.wait_cycles);
+                    __syncwarp();
+                    fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < D / 32; ++c) {
+                        float y[32];
+                        tmem_ld32(o_at + 32 * c, y);
+                        wait_ld(y);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) y[e] *= back;
+                        tmem_st32(o_at + 32 * c, y);
+                    }
+                    wait_st();
+                }
+            }
+            // (where V is so small against what O holds that its weights leave fp16, they must not leave fp32, for the sum's sake)
+            const int up2 = ve - E < -90 ? -90 : ve - E;
+            const float sub = (float)(P_SHIFT + up2) - m;
+            const qp_f2 f2 = qp_pack2(f, f), sub2 = qp_pack2(sub, sub);
+            qp_f2 sum = qp_pack2(0.f, 0.f), sum1 = sum;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t h[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float y0, y1;
+                    qp_unpack2(qp_fma2(qp_pack2(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), f2, sub2), y0, y1);
+                    y0 = ex2(y0);
+                    y1 = ex2(y1);
+                    if (e & 1) sum1 = qp_add2(sum1, qp_pack2(y0, y1));
+                    else sum = qp_add2(sum, qp_pack2(y0, y1));
+                    h[e] = half2_of(y0, y1);
+                }
+                tmem_st16(s_at + 16 * c, h);
+            }
+            float s0, s1;
+            qp_unpack2(qp_add2(sum, sum1), s0, s1);
+            l = fmaf(s0 + s1, pow2(-up2 - P_SHIFT), l);
+            wait_st();
+            fence_before();
+            arrive(&sh.p_full[t]);
+        }
+        // ---- the row's result
+        wait(sh, &sh.pv_done[t], (g - 1) & 1, a.wait_cycles);
+        __syncwarp();
+        fence_after();
+        const bool out = mine && !given_up(sh);
+        const float un = pow2(E - P_SHIFT);
+        float* part = a.part + ((int64_t)s.at * 2 + t) * C::PART;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+            float y[32];
+            tmem_ld32(o_at + 32 * c, y);
+            wait_ld(y);
+            if (out) {
+#pragma unroll
+                for (int e = 0; e < 32; e += 4) {
+                    const float4 o = make_float4(y[e] * un, y[e + 1] * un, y[e + 2] * un, y[e + 3] * un);
+                    if (!s.split) put_row<D>(a, s, r, 32 * c + e, o, m, l, bad);
+                    else __stcg(reinterpret_cast<float4*>(part + row * D + 32 * c + e), o);
+                }
+            }
+        }
+        if (s.split) {
+            if (out) {
+                __stcg(part + TILE * D + row, bad ? __int_as_float(0x7FC00000) : m);
+                __stcg(part + TILE * D + TILE + row, l);
+            }
+            const int parts = s.c1 - s.c0 + 1;
+            __threadfence();
+            group_sync(2 + t);
+            if (row == 0) {
+                unsigned* count = a.count + s.first_at * 2 + t;
+                sh.last[t] = atomicAdd(count, 1u) == (unsigned)(parts - 1);
+                if (sh.last[t]) *count = 0u;
+            }
+            group_sync(2 + t);
+            if (__all_sync(0xFFFFFFFFu, sh.last[t] != 0 && !given_up(sh))) {
+                __threadfence();
+                auto at = [&](int p) { return a.part + ((int64_t)(p ? 2 * (s.c0 + p) : s.first_at) * 2 + t) * C::PART; };
+                const int warp_row = row & ~31;
+                for (int k = 0; k < 32; ++k) {                   // a warp to a row
+                    const int64_t rr = (int64_t)s.tile * ROWS + t * TILE + warp_row + k;
+                    if (rr >= all) break;
+                    const int w = warp_row + k;
+                    float best = M_NONE;
+                    bool nan = false;
+                    for (int p = lane; p < parts; p += 32) {
+                        const float y = __ldcg(at(p) + TILE * D + w);
+                        nan |= !(y == y);
+                        best = fmaxf(best, y);
+                    }
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xFFFFFFFFu, best, o));
+                    nan = __any_sync(0xFFFFFFFFu, nan);
+                    float sl = 0.f;
+                    float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+                    for (int p = 0; p < parts; ++p) {
+                        const float* x = at(p);
+                        const float wt = ex2(__ldcg(x + TILE * D + w) - best);
+                        sl = fmaf(wt, __ldcg(x + TILE * D + TILE + w), sl);
+                        if (lane < D / 4) {
+                            const float4 y = __ldcg(reinterpret_cast<const float4*>(x + w * D) + lane);
+                            so.x = fmaf(wt, y.x, so.x); so.y = fmaf(wt, y.y, so.y); so.z = fmaf(wt, y.z, so.z); so.w = fmaf(wt, y.w, so.w);
+                        }
+                    }
+                    if (lane < D / 4) put_row<D>(a, s, rr, 4 * lane, so, best, sl, nan);
+                }
+            }
+        }
+        fence_before();
+    }
+}
+
+template <int D>
+__global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_args a)
+{
+    using C = Cfg<D>;
+    extern __shared__ char raw[];
+    __shared__ Shared sh;
+    char* smem = raw + ((1024u - (smem_of(raw) & 1023u)) & 1023u);
+    char* stages = smem + 2 * C::OPERAND;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    // ---- the work, and this block's run of it (every warp for itself)
+    int64_t W = 0;
+    for (int b = lane; b < a.rows.batch; b += 32) W += work_of(a, seq_of(a, b)) * a.heads;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) W += __shfl_xor_sync(0xFFFFFFFFu, W, o);
+    int64_t blocks = W / (MIN_RUN + HEAD);
+    blocks = blocks < 1 ? 1 : blocks < (int64_t)gridDim.x ? blocks : (int64_t)gridDim.x;
+    if (W == 0 || (int64_t)blockIdx.x >= blocks) return;
+    const int64_t begin = blockIdx.x * W / blocks, end = (blockIdx.x + 1ll) * W / blocks;
+
+    if (threadIdx.x == 0) {
+        for (int t = 0; t < 2; ++t) {
+            qp_stream::mbar_init(&sh.q_full[t], TILE);
+            qp_stream::mbar_init(&sh.kv_full[t], 128);
+            qp_stream::mbar_init(&sh.kv_empty[t], 1);
+            qp_stream::mbar_init(&sh.s_full[t], 1);
+            qp_stream::mbar_init(&sh.p_full[t], TILE);
+            qp_stream::mbar_init(&sh.pv_done[t], 1);
+        }
+        qp_stream::mbar_init(&sh.all_done, 1);
+        sh.give_up = 0u;
+        qp_stream::fence_barrier_init();
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_of(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    int64_t u = begin, base = 0;
+    int b = 0;
+    if (warp == 0) {                                             // the sequence that the run begins in
+        for (int64_t front = 0; ; b += 32) {
+            const int64_t mine = b + lane < a.rows.batch ? work_of(a, seq_of(a, b + lane)) * a.heads : 0;
+            int64_t x = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t y = __shfl_up_sync(0xFFFFFFFFu, x, o);
+                if (lane >= o) x += y;
+            }
+            const unsigned hit = __ballot_sync(0xFFFFFFFFu, begin >= front + x - mine && begin < front + x);
+            if (hit) {
+                const int at = __ffs(hit) - 1;
+                base = front + __shfl_sync(0xFFFFFFFFu, x - mine, at);
+                b += at;
+                break;
+            }
+            front += __shfl_sync(0xFFFFFFFFu, x, 31);
+            if (b + 32 >= a.rows.batch) break;                   // (never: begin < W)
+        }
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+
+    int g = 0, items = 0;
+    for (;;) {
+        if (warp == 0) list_parts(a, sh, u, end, begin, W, blocks, b, base);
+        __syncthreads();
+        if (warp < 8) softmax<D>(a, sh, smem, g);
+        else if (warp < 12) produce<D>(a, sh, stages, g);
+        else if (warp == 12 && lane == 0) multiply<D>(a, sh, smem, stages, g, items);
+        __syncwarp();
+        const bool more = sh.more != 0;
+        __syncthreads();                                         // the list is free
+        if (!more) break;
+    }
+    // all products have to be done before tensor memory goes back
+    if (warp == 12 && lane == 0) {
+        commit(&sh.all_done);
+        for (long long since = clock64(); !qp_stream::mbar_try_wait(&sh.all_done, 0u) && clock64() - since < QP_STREAM_TIMEOUT_CYCLES;) {}
+    }
+    if (threadIdx.x == 0 && given_up(sh)) atomicOr(a.status, QP_DEV_STREAM_TIMEOUT);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(sh.tmem) : "memory");
+}
+
+}  // namespace
+
+uint64_t qp_kv_chunk_part_bytes(int head_dim, int sm_count)
+{
+    return head_dim <= 128 ? (uint64_t)sm_count * 2 * 2 * TILE * (uint64_t)(head_dim + 2) * 4 : 0;
+}
+
+int32_t qp_kv_chunk_launch(qp_ctx* ctx, const qp_kv_attn_args& a, int head_dim, cudaStream_t s)
+{
+    static bool ready[2][QP_KV_MAX_DEVICES];
+    const void* f = head_dim == 64 ? reinterpret_cast<const void*>(kv_chunk_kernel<64>) : reinterpret_cast<const void*>(kv_chunk_kernel<128>);
+    const int smem = head_dim == 64 ? Cfg<64>::SMEM : Cfg<128>::SMEM;
+    bool* done = ctx->device < QP_KV_MAX_DEVICES ? &ready[head_dim == 128][ctx->device] : nullptr;
+    if (!done || !*done) {
+        if (cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess)
+            return qp_check_launch(ctx, "qp_kv_attention (shared memory)");
+        if (done) *done = true;
+    }
+    void* args[] = {const_cast<qp_kv_attn_args*>(&a)};
+    cudaLaunchKernel(f, dim3((unsigned)ctx->sm_count), dim3(THREADS), args, (size_t)smem, s);
+    ctx->launches += 1;
+    return qp_check_launch(ctx, "qp_kv_attention");
+}

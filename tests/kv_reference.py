@@ -53,12 +53,13 @@ def sequence(pool, pages, head, n, page_size, dim):
     return [tuple(a.reshape(-1, *a.shape[2:])[:n] for a in values(c, q)) for c, q in ((kc, kq), (vc, vq))]
 
 
-def attention_row(q, k, v, visible, scale, weight_eps, out_eps):
-    """(out, lse, bound of |error|) of one query over the rows of `sequence`, fp64; visible [n] truth values."""
+def attention_row(q, k, v, visible, scale, weight_eps, out_eps, halves=False):
+    """(out, lse, bound of |error|, of lse's) of one query over the rows of `sequence`, fp64; visible [n] truth values.  halves: for
+    the kernel that rounds the rows of K and V to fp16 first."""
     kv, klo, ks, _ = k
     vv, vlo, vs, vc = v
     if not visible.any():
-        return np.zeros(vv.shape[1] if vv.ndim == 2 else len(q)), -np.inf, np.zeros(len(q)), 0.0
+        return np.zeros(len(q)), -np.inf, np.zeros(len(q)), 0.0
     kv, klo, ks, vv, vs, vc = kv[visible], klo[visible], ks[visible], vv[visible], vs[visible], vc[visible]
     s = kv @ q * scale
     top = s.max()
@@ -73,7 +74,14 @@ def attention_row(q, k, v, visible, scale, weight_eps, out_eps):
     # 2^-25 / 16 of the largest scale; sums of up to n terms in fp32 add n / 8 steps at most (a lane sums an eighth of a warp's share).
     spread = np.abs(vv).max() + np.abs(out).max()
     n = len(s)
-    err = (2 * ds + 2.0 ** -20 + (n / 8 + 16) * 2.0 ** -24) * spread + weight_eps * (p * vs) @ vc / l + n * 15 * 2.0 ** -29 * vs.max() / l
+    weights = weight_eps * (p * vs) @ vc / l + n * 15 * 2.0 ** -29 * vs.max() / l
+    if halves:
+        # A row's value is rounded to fp16 (2^-11 of itself, or 2^-35 of its tile's largest) from a fused operation whose constant,
+        # lo - 2048 scale at most, is off by up to 2^-24 * 2048 scale; a weight p to fp16 too, or to 2^-30 of the values' power of two,
+        # which is below 2^-10 of their largest times 2^11.
+        ds += abs(scale) * (np.abs(kv) @ np.abs(q) * 2.0 ** -11 + np.abs(q).sum() * (2.0 ** -13 * ks + 2.0 ** -35 * np.abs(kv).max())).max()
+        weights = p @ (2.0 ** -10 * np.abs(vv) + (2.0 ** -13 * vs + 2.0 ** -35 * np.abs(vv).max())[:, None]) / l + n * 2.0 ** -28 * np.abs(vv).max() / l
+    err = (2 * ds + 2.0 ** -20 + (n / 8 + 16) * 2.0 ** -24) * spread + weights
     return out, top + np.log(l), err + out_eps * (np.abs(out) + err), 2 * ds + (n / 8 + 16) * 2.0 ** -23 + 2.0 ** -20 * (1 + abs(top))
 
 

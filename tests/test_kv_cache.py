@@ -226,6 +226,11 @@ def test_rows_are_those_of_the_token_calls(ctx, dim, dtype):
     assert np.array_equal(kq.reshape(160, 8).copy().view(np.float32), quant[:, [0, 2]])
 
 
+def halves(dtype, dim, rows):
+    """Whether these query rows to a cached head go through the kernel that takes K and V in fp16."""
+    return dtype == BF16 and dim <= 128 and rows >= 64
+
+
 def check_attention(ctx, cache, lens_k, slots, pos, start, q, window, got, lse, scale, rows_left=None):
     pool, table = cache.pool[0].cpu().numpy(), cache.table.cpu().numpy()
     group = q.shape[1] // cache.heads
@@ -248,7 +253,7 @@ def check_attention(ctx, cache, lens_k, slots, pos, start, q, window, got, lse, 
                 for g in range(group):
                     row, hq = int(start[b]) + i, h * group + g
                     out, e, bound, lb = ref.attention_row(qn[row, hq], k, v, seen, scale, 2.0 ** -11 if bf else 2.0 ** -21,
-                                                          torch.finfo(q.dtype).eps / 2)
+                                                          torch.finfo(q.dtype).eps / 2, halves(q.dtype, cache.head_dim, n * group))
                     off = np.abs(gn[row, hq] - out)
                     assert (off <= bound).all(), (b, i, h, g, float((off / bound).max()))
                     worst = max(worst, float((off / bound).max()))
@@ -360,7 +365,8 @@ def test_attention_of_odd_batches(ctx, dtype, new):
         for i in (0, new - 1):
             seen = (np.arange(222) <= pos[4] + i) & ((np.arange(222) < 32) | (np.arange(222) >= 48))
             r, hq = int(start[4]) + i, h * group + 1
-            o, e, bound, _ = ref.attention_row(qn[r, hq], k, v, seen, dim ** -0.5, 2.0 ** -11, torch.finfo(dtype).eps / 2)
+            o, e, bound, _ = ref.attention_row(qn[r, hq], k, v, seen, dim ** -0.5, 2.0 ** -11, torch.finfo(dtype).eps / 2,
+                                               halves(dtype, dim, new * group))
             assert (np.abs(gn[r, hq] - o) <= bound).all()
 
 
@@ -410,6 +416,54 @@ def test_attention_of_a_long_sequence(ctx):
     lse = torch.empty(6, heads * group, device="cuda")
     out = ctx.qp_kv_attention(cache, batch, q, plan, lse=lse)
     check_attention(ctx, cache, lens, range(6), pos, np.arange(7), q, 0, out, lse, plan.scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim,group,window", [(128, 4, 0), (64, 2, 0), (128, 3, 700)])
+def test_attention_of_mixed_batches(ctx, dim, group, window):
+    """Chunks of prompts, drafts and single tokens in one batch; chunks whose work is cut between many blocks."""
+    rng = np.random.default_rng(12)
+    lens, new, heads = [3000, 900, 64, 2000, 1, 777], [500, 1, 64, 5, 1, 130], 2
+    cache = make(rng, lens, heads, dim, 32)
+    fill(ctx, rng, cache, lens, dtype=BF16)
+    start = np.concatenate(([0], np.cumsum(new)))
+    total = int(start[-1])
+    q = torch.from_numpy(rng.standard_normal((total, heads * group, dim)).astype(np.float32)).cuda().to(BF16)
+    pos = [n - m for n, m in zip(lens, new)]
+    batch = qp.KVBatch(ints(pos), start=ints(start), tokens=total, max_new=500)
+    plan = ctx.qp_kv_attention_plan(cache, heads * group, window, scale=-0.07)
+    lse = torch.empty(total, heads * group, device="cuda")
+    out = ctx.qp_kv_attention(cache, batch, q, plan, lse=lse)
+    assert ctx.qp_get_status() == 0
+    check_attention(ctx, cache, lens, range(6), pos, start, q, window, out, lse, plan.scale)
+    zero = qp.KVAttention(plan.work, heads * group, window, 0.0)     # all keys alike
+    ctx.qp_kv_attention(cache, batch, q, zero, out=out, lse=lse)
+    check_attention(ctx, cache, lens, range(6), pos, start, q, window, out, lse, 0.0)
+
+
+@pytest.mark.gpu
+def test_a_wait_that_runs_out(ctx):
+    """The chunk kernel's waits are bounded: one that gives up reports it, and the context and the plan stay usable."""
+    rng = np.random.default_rng(13)
+    lens, heads, group, dim = [2500, 1300], 2, 4, 128
+    cache = make(rng, lens, heads, dim, 16)
+    fill(ctx, rng, cache, lens, dtype=BF16)
+    q = torch.from_numpy(rng.standard_normal((800, heads * group, dim)).astype(np.float32)).cuda().to(BF16)
+    batch = qp.KVBatch(ints([2000, 1000]), start=ints([0, 500, 800]), tokens=800, max_new=500)
+    plan = ctx.qp_kv_attention_plan(cache, heads * group)
+    good = ctx.qp_kv_attention(cache, batch, q, plan)
+    assert ctx.qp_get_status() == 0
+    ctx.qp_set_wait_limit_for_testing(tile_wait_cycles=0)
+    try:
+        ctx.qp_kv_attention(cache, batch, q, plan)
+        with pytest.raises(qp.QuantPipeError) as e:
+            ctx.qp_get_status()
+        assert e.value.status == qp.QP_ERR_TIMEOUT
+    finally:
+        ctx.qp_set_wait_limit_for_testing()
+    assert ctx.qp_get_status() == 0 and int(plan.work[:4096 * 4].count_nonzero()) == 0
+    assert torch.equal(ctx.qp_kv_attention(cache, batch, q, plan), good)
+    assert ctx.qp_get_status() == 0
 
 
 @pytest.mark.gpu
