@@ -669,6 +669,16 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
     }
 }
 
+__device__ __forceinline__ void block_sync() { asm volatile("bar.sync 0;" ::: "memory"); }
+// behind a list of parts: whether there is another, once nobody reads this one any more
+__device__ __forceinline__ bool more_parts(const Shared& sh)
+{
+    __syncwarp();
+    const bool more = *(const volatile int*)&sh.more != 0;
+    block_sync();
+    return more;
+}
+
 template <int D>
 __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_args a)
 {
@@ -732,17 +742,29 @@ __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_a
     __syncthreads();
     fence_after();
 
-    int g = 0, items = 0;
-    for (;;) {
-        if (warp == 0) list_parts(a, sh, u, end, begin, W, blocks, b, base);
-        __syncthreads();
-        if (warp < 8) softmax<D>(a, sh, smem, g);
-        else if (warp < 12) produce<D>(a, sh, stages, g);
-        else if (warp == 12 && lane == 0) multiply<D>(a, sh, smem, stages, g, items);
-        __syncwarp();
-        const bool more = sh.more != 0;
-        __syncthreads();                                         // the list is free
-        if (!more) break;
+    // Registers by role: 2 * 128 * 184 + 128 * 88 + 128 * 40 are fewer than the block's 512 * 128.  (A loop for each role, so that each
+    // is compiled for its own number.)
+    int g = 0;
+    if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+        do {
+            if (warp == 0) list_parts(a, sh, u, end, begin, W, blocks, b, base);
+            block_sync();
+            softmax<D>(a, sh, smem, g);
+        } while (more_parts(sh));
+    } else if (warp < 12) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        do {
+            block_sync();
+            produce<D>(a, sh, stages, g);
+        } while (more_parts(sh));
+    } else {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        int items = 0;
+        do {
+            block_sync();
+            if (warp == 12 && lane == 0) multiply<D>(a, sh, smem, stages, g, items);
+        } while (more_parts(sh));
     }
     // all products have to be done before tensor memory goes back
     if (warp == 12 && lane == 0) {
