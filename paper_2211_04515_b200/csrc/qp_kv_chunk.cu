@@ -31,6 +31,7 @@ QP_CK_UNIT
 namespace {
 
 constexpr int THREADS = 512, TILE = 128, ROWS = 2 * TILE;
+constexpr int HALF = 64;                         // keys of a step of softmax and products
 constexpr int HEAD = 2;                          // what an item costs beside its key tiles, in key tiles
 constexpr int MIN_RUN = 4;                       // key tiles that are worth a block
 constexpr int SEGS = 32;                         // parts of items that are listed at a time
@@ -60,21 +61,30 @@ __host__ __device__ constexpr uint32_t shape_of(int n, bool b_mn_major)
 {
     return 1u << 4 | (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n / 8) << 17 | (uint32_t)(128 / 16) << 24;
 }
+// (called by a whole warp, issued by one lane: what the instructions take in uniform registers stays uniform)
+__device__ __forceinline__ bool leader()
+{
+    uint32_t e;
+    asm volatile("{.reg .pred p; elect.sync _|p, 0xFFFFFFFF; selp.b32 %0, 1, 0, p;}" : "=r"(e));
+    return e != 0u;
+}
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add)
 {
-    asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d), "l"(a), "l"(b),
-                 "r"(shape), "r"((uint32_t)add)
-                 : "memory");
+    if (leader())
+        asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;}" ::"r"(d), "l"(a), "l"(b),
+                     "r"(shape), "r"((uint32_t)add)
+                     : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add)
 {
-    asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d), "r"(a), "l"(b),
-                 "r"(shape), "r"((uint32_t)add)
-                 : "memory");
+    if (leader())
+        asm volatile("{.reg .pred p; setp.ne.b32 p, %4, 0; tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;}" ::"r"(d), "r"(a), "l"(b),
+                     "r"(shape), "r"((uint32_t)add)
+                     : "memory");
 }
 __device__ __forceinline__ void commit(uint64_t* bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_of(bar)) : "memory");
+    if (leader()) asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_of(bar)) : "memory");
 }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -154,7 +164,7 @@ struct Seg {
 };
 
 struct Shared {
-    uint64_t q_full[2], kv_full[2], kv_empty[2], s_full[2], p_full[2], pv_done[2], all_done;
+    uint64_t q_full[2], kv_full[2], kv_empty[2], s_full[2][2], p_full[2][2], pv_done[2][2], all_done;
     uint32_t tmem, give_up;
     int n_segs, more;
     float kinv[2];                               // per stage: what takes K's scaled values back
@@ -279,42 +289,39 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
     for (int i = 0; i < sh.n_segs; ++i) {
         const Seg& s = sh.segs[i];
         const int held = s.pos + s.n, units = s.u1 - s.u0;
-        uint4 k[L], v[L];
-        float4 quant;
-        // what the tile needs from memory, into registers
-        auto load = [&](int u) {
-            const int first = s.s0 + 8 * u;
-            int64_t place = -1;
-            if (lane < 8) {                                      // lane i of each warp: slice i
-                const int sl = first + lane, pg = sl / a.slices;
-                const int64_t at = (int64_t)sl * QP_KV_SLICE;
-                if (at < held) {
-                    const int page = qp_kv_page(a.pages, s.slot, pg * a.pages.page_size);
-                    if (page >= 0) place = (((int64_t)page * a.heads + s.head) * a.slices + (sl - pg * a.slices)) * C::SB;
-                    else atomicOr(a.status, QP_DEV_KV_RANGE);
-                }
+        // what a tile needs from memory, in registers: asked for one tile ahead, its places two
+        struct Raw { uint4 k[L], v[L]; float4 quant; unsigned there; } raw[2];
+        int64_t place = -1;
+        auto look_up = [&](int u) {                              // lane i < 8 of each warp: slice i
+            const int sl = s.s0 + 8 * u + lane, pg = sl / a.slices;
+            place = -1;
+            if (lane < 8 && u < s.u1 && (int64_t)sl * QP_KV_SLICE < held) {
+                const int page = qp_kv_page(a.pages, s.slot, pg * a.pages.page_size);
+                if (page >= 0) place = (((int64_t)page * a.heads + s.head) * a.slices + (sl - pg * a.slices)) * C::SB;
+                else atomicOr(a.status, QP_DEV_KV_RANGE);
             }
+        };
+        auto load = [&](Raw& x, int u) {
 #pragma unroll
             for (int l = 0; l < L; ++l) {
-                const int sl = (l * 128 + p) / PER;
-                const int64_t at = __shfl_sync(0xFFFFFFFFu, place, sl);
-                const char* x = a.pool + at + row * S::ROW + piece * 16;
-                k[l] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(x)) : make_uint4(0, 0, 0, 0);
-                v[l] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(x + S::V)) : make_uint4(0, 0, 0, 0);
+                const int64_t at = __shfl_sync(0xFFFFFFFFu, place, (l * 128 + p) / PER);
+                const char* from = a.pool + at + row * S::ROW + piece * 16;
+                x.k[l] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
+                x.v[l] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(from + S::V)) : make_uint4(0, 0, 0, 0);
             }
             const int64_t mine = __shfl_sync(0xFFFFFFFFu, place, p / QP_KV_SLICE);
-            quant = make_float4(0.f, 0.f, 0.f, 0.f);
-            const bool there = mine >= 0 && first * QP_KV_SLICE + p < held;
+            x.quant = make_float4(0.f, 0.f, 0.f, 0.f);
+            const bool there = mine >= 0 && (s.s0 + 8 * u) * QP_KV_SLICE + p < held;
             if (there) {
                 const float2 kq = __ldg(reinterpret_cast<const float2*>(a.pool + mine + S::KQ + p % QP_KV_SLICE * 8));
                 const float2 vq = __ldg(reinterpret_cast<const float2*>(a.pool + mine + S::VQ + p % QP_KV_SLICE * 8));
-                quant = make_float4(kq.x, kq.y, vq.x, vq.y);
+                x.quant = make_float4(kq.x, kq.y, vq.x, vq.y);
             }
-            return __ballot_sync(0xFFFFFFFFu, there);
+            x.there = __ballot_sync(0xFFFFFFFFu, there);
         };
-        unsigned there = load(s.u0);
-        for (int u = 0; u < units; ++u, ++g) {
+        auto convert = [&](const Raw& x) {
             const int st = g & 1;
+            const float4 quant = x.quant;
             // powers of two for the tile
             float ka = fmaxf(fabsf(quant.x), fabsf(fmaf(15.f, quant.y, quant.x))), va = fmaxf(fabsf(quant.z), fabsf(fmaf(15.f, quant.w, quant.z)));
 #pragma unroll
@@ -345,29 +352,42 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
                     // a nibble under 128's (or 2048's) exponent is 128 + code: lo + scale * code in one fused operation
                     const float sc = q.y * f, lo = q.x * f;
                     const qp_f2 s2 = qp_pack2(sc, sc), c2 = qp_pack2(fmaf(-128.f, sc, lo), fmaf(-2048.f, sc, lo));
-                    const uint4 raw = h ? v[l] : k[l];
-                    const unsigned w4[4] = {raw.x, raw.y, raw.z, raw.w};
+                    const uint4 codes = h ? x.v[l] : x.k[l];
+                    const unsigned w4[4] = {codes.x, codes.y, codes.z, codes.w};
                     char* panel = to + h * C::OPERAND + (D == 128 ? (piece >> 1) * (TILE * 128) : 0) + key * 128;
                     const int c0 = D == 128 ? 4 * (piece & 1) : 4 * piece;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const unsigned x[4] = {w4[w] << 16, w4[w] << 8, w4[w], w4[w] >> 8};   // bits 16..19: codes 0, 2, 4, 6
-                        const unsigned y[4] = {w4[w] << 8, w4[w], w4[w] >> 8, w4[w] >> 16};   // bits 12..15: codes 1, 3, 5, 7
+                        const unsigned even[4] = {w4[w] << 16, w4[w] << 8, w4[w], w4[w] >> 8};   // bits 16..19: codes 0, 2, 4, 6
+                        const unsigned odd[4] = {w4[w] << 8, w4[w], w4[w] >> 8, w4[w] >> 16};    // bits 12..15: codes 1, 3, 5, 7
                         uint4 out;
                         unsigned* o = &out.x;
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            o[e] = half2_of(qp_fma2(qp_pack2(__uint_as_float((x[e] & 0x000F0000u) | 0x43000000u),
-                                                             __uint_as_float((y[e] & 0x0000F000u) | 0x45000000u)), s2, c2));
+                            o[e] = half2_of(qp_fma2(qp_pack2(__uint_as_float((even[e] & 0x000F0000u) | 0x43000000u),
+                                                             __uint_as_float((odd[e] & 0x0000F000u) | 0x45000000u)), s2, c2));
                         *reinterpret_cast<uint4*>(panel + (((c0 + w) ^ (key & 7)) << 4)) = out;
                     }
                 }
             }
             if (p == 0) { sh.kinv[st] = pow2(ke); sh.ve[st] = ve; }
-            if (lane == 0) sh.valid[st][p >> 5] = there;
+            if (lane == 0) sh.valid[st][p >> 5] = x.there;
             fence_operands();
             arrive(&sh.kv_full[st]);
-            if (u + 1 < units) there = load(s.u0 + u + 1);
+            ++g;
+        };
+        look_up(s.u0);
+        load(raw[0], s.u0);
+        look_up(s.u0 + 1);
+        for (int u = 0; u < units; u += 2) {
+            load(raw[1], s.u0 + u + 1);                          // (behind the last: nothing)
+            look_up(s.u0 + u + 2);
+            convert(raw[0]);
+            if (u + 1 < units) {
+                load(raw[0], s.u0 + u + 2);
+                look_up(s.u0 + u + 3);
+                convert(raw[1]);
+            }
         }
     }
 }
@@ -378,15 +398,21 @@ template <int D>
 __device__ __forceinline__ void multiply(const qp_kv_attn_args& a, Shared& sh, char* q_at, char* stages, int& g, int& items)
 {
     using C = Cfg<D>;
-    constexpr uint32_t S_SHAPE = shape_of(TILE, false), O_SHAPE = shape_of(D, true);
-    const uint32_t q0 = smem_of(q_at), kv0 = smem_of(stages), tm = sh.tmem;
-    auto scores = [&](int t, int st) {
+    constexpr uint32_t S_SHAPE = shape_of(HALF, false), O_SHAPE = shape_of(D, true);
+    const uint32_t tm = sh.tmem;
+    // descriptors move on by 16-byte units of the address
+    const uint64_t q_desc = operand_at(smem_of(q_at), 16), k_desc = operand_at(smem_of(stages), 16),
+                   v_desc = operand_at(smem_of(stages) + C::OPERAND, TILE * 128);
+    // query tile t against half h of the key tile in stage st
+    auto scores = [&](int t, int st, int h) {
+        const uint64_t q = q_desc + (uint32_t)(t * (C::OPERAND / 16)), k = k_desc + (uint32_t)(st * (2 * C::OPERAND / 16) + h * (HALF * 128 / 16));
+        const uint32_t to = tm + t * TILE + h * HALF;
 #pragma unroll
         for (int s = 0; s < D / 16; ++s) {
-            const uint32_t in = (uint32_t)(s >> 2) * (TILE * 128) + (uint32_t)(s & 3) * 32;
-            mma_ss(tm + t * TILE, operand_at(q0 + t * C::OPERAND + in, 16), operand_at(kv0 + st * 2 * C::OPERAND + in, 16), S_SHAPE, s > 0);
+            const uint32_t in = (uint32_t)(s >> 2) * (TILE * 128 / 16) + (uint32_t)(s & 3) * 2;
+            mma_ss(to, q + in, k + in, S_SHAPE, s > 0);
         }
-        commit(&sh.s_full[t]);
+        commit(&sh.s_full[t][h]);
     };
     for (int i = 0; i < sh.n_segs; ++i, ++items) {
         const int units = sh.segs[i].u1 - sh.segs[i].u0;
@@ -394,24 +420,31 @@ __device__ __forceinline__ void multiply(const qp_kv_attn_args& a, Shared& sh, c
         for (int t = 0; t < 2; ++t) {
             wait(sh, &sh.q_full[t], items & 1, a.wait_cycles);
             fence_after();
-            scores(t, g & 1);
+            scores(t, g & 1, 0);
         }
+        for (int t = 0; t < 2; ++t) scores(t, g & 1, 1);
         for (int u = 0; u < units; ++u, ++g) {
             const int st = g & 1;
-            for (int t = 0; t < 2; ++t) {
-                wait(sh, &sh.p_full[t], g & 1, a.wait_cycles);
-                fence_after();
-#pragma unroll
-                for (int s = 0; s < TILE / 16; ++s)
-                    mma_ts(tm + 2 * TILE + t * TILE, tm + t * TILE + s * 8, operand_at(kv0 + (st * 2 + 1) * C::OPERAND + s * 2048, TILE * 128), O_SHAPE,
-                           u > 0 || s > 0);
-                commit(&sh.pv_done[t]);
-                if (t == 1) commit(&sh.kv_empty[st]);
-                if (u + 1 < units) {                             // the next scores take the place of the weights just used
-                    if (t == 0) wait(sh, &sh.kv_full[st ^ 1], ((g + 1) >> 1) & 1, a.wait_cycles);
-                    wait(sh, &sh.pv_done[t], g & 1, a.wait_cycles);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+                for (int t = 0; t < 2; ++t) {
+                    wait(sh, &sh.p_full[t][h], g & 1, a.wait_cycles);
                     fence_after();
-                    scores(t, st ^ 1);
+                    const uint64_t v = v_desc + (uint32_t)(st * (2 * C::OPERAND / 16) + h * (HALF * 128 / 16));
+                    const uint32_t to = tm + 2 * TILE + t * TILE, from = tm + t * TILE + h * HALF;
+                    const bool add = u > 0 || h > 0;
+#pragma unroll
+                    for (int s = 0; s < HALF / 16; ++s) mma_ts(to, from + s * 8, v + (uint32_t)(s * (2048 / 16)), O_SHAPE, add || s > 0);
+                    commit(&sh.pv_done[t][h]);
+                }
+                if (h == 1) commit(&sh.kv_empty[st]);
+                if (u + 1 < units) {                             // the next tile's scores take the place of the weights just used
+                    if (h == 0) wait(sh, &sh.kv_full[st ^ 1], ((g + 1) >> 1) & 1, a.wait_cycles);
+                    for (int t = 0; t < 2; ++t) {
+                        wait(sh, &sh.pv_done[t][h], g & 1, a.wait_cycles);
+                        fence_after();
+                        scores(t, st ^ 1, h);
+                    }
                 }
             }
         }
@@ -515,89 +548,92 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         int E = -1000;                                           // O holds sums of p * v * 2^(P_SHIFT - E)
         for (int u = s.u0; u < s.u1; ++u, ++g) {
             const int st = g & 1;
-            const int64_t t0 = ((int64_t)s.s0 + 8 * u) * QP_KV_SLICE;
             wait(sh, &sh.kv_full[st], (g >> 1) & 1, a.wait_cycles);      // (long there: for what the producers say of the tile)
-            wait(sh, &sh.s_full[t], g & 1, a.wait_cycles);
-            __syncwarp();
-            fence_after();
-            float x[TILE];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, x + 32 * c);
             const float f = fmaxf(kf * sh.kinv[st], 1e-37f);     // (positive, so that -inf stays)
             const int ve = sh.ve[st];
-            wait_ld(x);
-            const unsigned valid = sh.valid[st][0] & sh.valid[st][1] & sh.valid[st][2] & sh.valid[st][3];
-            if (valid != 0xFFFFFFFFu || t0 < all_lo || t0 + TILE > all_hi) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int64_t up = hi - t0 - 32 * c, down = a.window > 0 ? hi - a.window - t0 - 32 * c : -1;   // keys (down, up]
-                    unsigned seen = sh.valid[st][c];
-                    seen &= up < 0 ? 0u : up >= 31 ? 0xFFFFFFFFu : (2u << up) - 1u;
-                    seen &= down < 0 ? 0xFFFFFFFFu : down >= 31 ? 0u : ~((2u << down) - 1u);
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) x[32 * c + e] = seen >> e & 1u ? x[32 * c + e] : -inf;
-                }
-            }
-            float top4[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-            for (int c = 4; c < TILE; c += 8)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top4[e] = c + 4 + e < TILE ? qp_max3(top4[e], x[c + e], x[c + 4 + e]) : fmaxf(top4[e], x[c + e]);
-            const float top = fmaxf(qp_max3(top4[0], top4[1], top4[2]), top4[3]) * f;
-            if (__any_sync(0xFFFFFFFFu, top > m + M_SLACK || ve > E)) {     // rare: a new reference
-                const float next = fmaxf(m, top);
-                float back = ex2(m - next);
-                m = next;
-                l *= back;
-                if (ve > E) {
-                    back *= E < -999 ? 0.f : pow2(E - ve);
-                    E = ve;
-                }
-                if (u > s.u0) {
-                    wait(sh, &sh.pv_done[t], (g - 1) & 1, a.wait_cycles);
-                    __syncwarp();
-                    fence_after();
 #pragma unroll 1
-                    for (int c = 0; c < D / 32; ++c) {
-                        float y[32];
-                        tmem_ld32(o_at + 32 * c, y);
-                        wait_ld(y);
+            for (int h = 0; h < 2; ++h) {
+                const int64_t t0 = ((int64_t)s.s0 + 8 * u) * QP_KV_SLICE + h * HALF;
+                wait(sh, &sh.s_full[t][h], g & 1, a.wait_cycles);
+                __syncwarp();
+                fence_after();
+                float x[HALF];
+                tmem_ld32(s_at + h * HALF, x);
+                tmem_ld32(s_at + h * HALF + 32, x + 32);
+                const unsigned valid[2] = {sh.valid[st][2 * h], sh.valid[st][2 * h + 1]};
+                wait_ld(x);
+                if ((valid[0] & valid[1]) != 0xFFFFFFFFu || t0 < all_lo || t0 + HALF > all_hi) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) y[e] *= back;
-                        tmem_st32(o_at + 32 * c, y);
+                    for (int c = 0; c < 2; ++c) {
+                        const int64_t up = hi - t0 - 32 * c, down = a.window > 0 ? hi - a.window - t0 - 32 * c : -1;   // keys (down, up]
+                        unsigned seen = valid[c];
+                        seen &= up < 0 ? 0u : up >= 31 ? 0xFFFFFFFFu : (2u << up) - 1u;
+                        seen &= down < 0 ? 0xFFFFFFFFu : down >= 31 ? 0u : ~((2u << down) - 1u);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[32 * c + e] = seen >> e & 1u ? x[32 * c + e] : -inf;
                     }
-                    wait_st();
                 }
-            }
-            // (where V is so small against what O holds that its weights leave fp16, they must not leave fp32, for the sum's sake)
-            const int up2 = ve - E < -90 ? -90 : ve - E;
-            const float sub = (float)(P_SHIFT + up2) - m;
-            const qp_f2 f2 = qp_pack2(f, f), sub2 = qp_pack2(sub, sub);
-            qp_f2 sum = qp_pack2(0.f, 0.f), sum1 = sum;
+                float top4[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t h[16];
+                for (int c = 4; c < HALF; c += 8)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float y0, y1;
-                    qp_unpack2(qp_fma2(qp_pack2(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), f2, sub2), y0, y1);
-                    y0 = ex2(y0);
-                    y1 = ex2(y1);
-                    if (e & 1) sum1 = qp_add2(sum1, qp_pack2(y0, y1));
-                    else sum = qp_add2(sum, qp_pack2(y0, y1));
-                    h[e] = half2_of(y0, y1);
+                    for (int e = 0; e < 4; ++e) top4[e] = c + 4 + e < HALF ? qp_max3(top4[e], x[c + e], x[c + 4 + e]) : fmaxf(top4[e], x[c + e]);
+                const float top = fmaxf(qp_max3(top4[0], top4[1], top4[2]), top4[3]) * f;
+                if (__any_sync(0xFFFFFFFFu, top > m + M_SLACK || ve > E)) {     // rare: a new reference
+                    const float next = fmaxf(m, top);
+                    float back = ex2(m - next);
+                    m = next;
+                    l *= back;
+                    if (ve > E) {
+                        back *= E < -999 ? 0.f : pow2(E - ve);
+                        E = ve;
+                    }
+                    if (u > s.u0 || h > 0) {
+                        wait(sh, &sh.pv_done[t][h ^ 1], (h ? g : g - 1) & 1, a.wait_cycles);      // of the half before
+                        __syncwarp();
+                        fence_after();
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            float y[32];
+                            tmem_ld32(o_at + 32 * c, y);
+                            wait_ld(y);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) y[e] *= back;
+                            tmem_st32(o_at + 32 * c, y);
+                        }
+                        wait_st();
+                    }
                 }
-                tmem_st16(s_at + 16 * c, h);
+                // (where V is so small against what O holds that its weights leave fp16, they must not leave fp32, for the sum's sake)
+                const int up2 = ve - E < -90 ? -90 : ve - E;
+                const float sub = (float)(P_SHIFT + up2) - m;
+                const qp_f2 f2 = qp_pack2(f, f), sub2 = qp_pack2(sub, sub);
+                qp_f2 sum = qp_pack2(0.f, 0.f), sum1 = sum;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t w[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        float y0, y1;
+                        qp_unpack2(qp_fma2(qp_pack2(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), f2, sub2), y0, y1);
+                        y0 = ex2(y0);
+                        y1 = ex2(y1);
+                        if (e & 1) sum1 = qp_add2(sum1, qp_pack2(y0, y1));
+                        else sum = qp_add2(sum, qp_pack2(y0, y1));
+                        w[e] = half2_of(y0, y1);
+                    }
+                    tmem_st16(s_at + h * HALF + 16 * c, w);
+                }
+                float s0, s1;
+                qp_unpack2(qp_add2(sum, sum1), s0, s1);
+                l = fmaf(s0 + s1, pow2(-up2 - P_SHIFT), l);
+                wait_st();
+                fence_before();
+                arrive(&sh.p_full[t][h]);
             }
-            float s0, s1;
-            qp_unpack2(qp_add2(sum, sum1), s0, s1);
-            l = fmaf(s0 + s1, pow2(-up2 - P_SHIFT), l);
-            wait_st();
-            fence_before();
-            arrive(&sh.p_full[t]);
         }
         // ---- the row's result
-        wait(sh, &sh.pv_done[t], (g - 1) & 1, a.wait_cycles);
+        wait(sh, &sh.pv_done[t][1], (g - 1) & 1, a.wait_cycles);
         __syncwarp();
         fence_after();
         const bool out = mine && !given_up(sh);
@@ -687,7 +723,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_a
     __shared__ Shared sh;
     char* smem = raw + ((1024u - (smem_of(raw) & 1023u)) & 1023u);
     char* stages = smem + 2 * C::OPERAND;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = __shfl_sync(0xFFFFFFFFu, (int)threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
 
     // ---- the work, and this block's run of it (every warp for itself)
     int64_t W = 0;
@@ -704,9 +740,11 @@ __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_a
             qp_stream::mbar_init(&sh.q_full[t], TILE);
             qp_stream::mbar_init(&sh.kv_full[t], 128);
             qp_stream::mbar_init(&sh.kv_empty[t], 1);
-            qp_stream::mbar_init(&sh.s_full[t], 1);
-            qp_stream::mbar_init(&sh.p_full[t], TILE);
-            qp_stream::mbar_init(&sh.pv_done[t], 1);
+            for (int h = 0; h < 2; ++h) {
+                qp_stream::mbar_init(&sh.s_full[t][h], 1);
+                qp_stream::mbar_init(&sh.p_full[t][h], TILE);
+                qp_stream::mbar_init(&sh.pv_done[t][h], 1);
+            }
         }
         qp_stream::mbar_init(&sh.all_done, 1);
         sh.give_up = 0u;
@@ -742,32 +780,31 @@ __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_a
     __syncthreads();
     fence_after();
 
-    // Registers by role: 2 * 128 * 184 + 128 * 88 + 128 * 40 are fewer than the block's 512 * 128.  (A loop for each role, so that each
+    // Registers by role: 2 * 128 * 128 + 128 * 160 + 128 * 96 are the block's 512 * 128.  (A loop for each role, so that each
     // is compiled for its own number.)
     int g = 0;
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
         do {
             if (warp == 0) list_parts(a, sh, u, end, begin, W, blocks, b, base);
             block_sync();
             softmax<D>(a, sh, smem, g);
         } while (more_parts(sh));
     } else if (warp < 12) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
         do {
             block_sync();
             produce<D>(a, sh, stages, g);
         } while (more_parts(sh));
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
         int items = 0;
         do {
             block_sync();
-            if (warp == 12 && lane == 0) multiply<D>(a, sh, smem, stages, g, items);
+            if (warp == 12) multiply<D>(a, sh, smem, stages, g, items);
         } while (more_parts(sh));
     }
     // all products have to be done before tensor memory goes back
-    if (warp == 12 && lane == 0) {
+    if (warp == 12) {
         commit(&sh.all_done);
         for (long long since = clock64(); !qp_stream::mbar_try_wait(&sh.all_done, 0u) && clock64() - since < QP_STREAM_TIMEOUT_CYCLES;) {}
     }
