@@ -149,7 +149,12 @@ __device__ __forceinline__ unsigned half2_of(qp_f2 v)
     qp_unpack2(v, a, b);
     return half2_of(a, b);
 }
-__device__ __forceinline__ void arrive(uint64_t* bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_of(bar)) : "memory"); }
+// a warp's arrival, for all that its lanes did before
+__device__ __forceinline__ void arrive(uint64_t* bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_of(bar)) : "memory");
+}
 template <int ID> __device__ __forceinline__ void group_sync() { asm volatile("bar.sync %0, 128;" ::"n"(ID) : "memory"); }
 __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e < -126 ? 1 : e > 127 ? 254 : e + 127) << 23); }
@@ -191,18 +196,21 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
     q.tiles = q.n <= 0 || q.pos < 0 || rows < a.many ? 0 : (int)((rows + ROWS - 1) / ROWS);
     return q;
 }
-// slices [first, first + 8 * returned) hold the keys that rows tile * ROWS .. see
+// slices [first, first + 8 * returned) hold the keys that rows tile * ROWS .. see (counts of rows and of keys fit 32 bits)
 __device__ __forceinline__ int tiles_of(const qp_kv_attn_args& a, const Seq& q, int tile, int& first)
 {
-    const int64_t most = (int64_t)a.pages.max_pages * a.pages.page_size;
-    const int64_t r0 = (int64_t)tile * ROWS, all = (int64_t)q.n * a.group, r1 = r0 + ROWS < all ? r0 + ROWS : all;
-    int64_t end = (int64_t)q.pos + (r1 - 1) / a.group + 1, lo = a.window > 0 ? (int64_t)q.pos + r0 / a.group - a.window + 1 : 0;
-    if (end > most) end = most;
-    if (lo < 0) lo = 0;
-    if (lo > end) lo = end;
+    const unsigned most = (unsigned)a.pages.max_pages * (unsigned)a.pages.page_size, group = (unsigned)a.group;
+    const unsigned r0 = (unsigned)tile * ROWS, all = (unsigned)q.n * group, r1 = r0 + ROWS < all ? r0 + ROWS : all;
+    const unsigned end0 = (unsigned)q.pos + (r1 - 1) / group + 1u, end = end0 < most ? end0 : most;
+    unsigned lo = 0u;
+    if (a.window > 0) {
+        const unsigned at = (unsigned)q.pos + r0 / group + 1u;
+        lo = at > (unsigned)a.window ? at - (unsigned)a.window : 0u;
+        if (lo > end) lo = end;
+    }
     first = (int)(lo / QP_KV_SLICE);
-    const int64_t slices = (end + QP_KV_SLICE - 1) / QP_KV_SLICE - first;
-    return slices < 1 ? 1 : (int)((slices + TILE / QP_KV_SLICE - 1) / (TILE / QP_KV_SLICE));
+    const int slices = (int)((end + QP_KV_SLICE - 1) / QP_KV_SLICE) - first;
+    return slices < 1 ? 1 : (slices + TILE / QP_KV_SLICE - 1) / (TILE / QP_KV_SLICE);
 }
 __device__ __forceinline__ int64_t work_of(const qp_kv_attn_args& a, const Seq& q)      // of one head
 {
@@ -455,10 +463,10 @@ __device__ __forceinline__ void multiply(const qp_kv_attn_args& a, Shared& sh, c
 
 // this row's out and lse
 template <int D>
-__device__ __forceinline__ void put_row(const qp_kv_attn_args& a, const Seg& s, int64_t r, int d, float4 o, float m, float l, bool bad)
+__device__ __forceinline__ void put_row(const qp_kv_attn_args& a, const Seg& s, int r, int d, float4 o, float m, float l, bool bad)
 {
     const int64_t token = s.row0 + r / a.group;
-    const int h = s.head * a.group + (int)(r % a.group);
+    const int h = s.head * a.group + r % a.group;
     const float nan = __int_as_float(0x7FC00000);
     float v[4] = {o.x, o.y, o.z, o.w};
     unsigned short x[4];
@@ -482,7 +490,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
     const float inf = __int_as_float(0x7F800000);
     for (int i = 0; i < sh.n_segs; ++i) {
         const Seg& s = sh.segs[i];
-        const int64_t r = (int64_t)s.tile * ROWS + t * TILE + row, all = (int64_t)s.n * a.group;
+        const int r = s.tile * ROWS + t * TILE + row, all = s.n * a.group;       // (tokens * q_heads is below 2^31 - 4096)
         const bool mine = r < all;
         // ---- the query row, scaled, into shared memory
         float kf;
@@ -490,7 +498,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         {
             uint4 x[D / 8];
             const unsigned short* from = static_cast<const unsigned short*>(a.q);
-            if (mine) from += (s.row0 + r / a.group) * a.qt + (int64_t)(s.head * a.group + (int)(r % a.group)) * a.qh;
+            if (mine) from += (int64_t)(s.row0 + r / a.group) * a.qt + (int64_t)(s.head * a.group + r % a.group) * a.qh;
             if (!mine) {
 #pragma unroll
                 for (int c = 0; c < D / 8; ++c) x[c] = make_uint4(0, 0, 0, 0);
@@ -539,11 +547,12 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
             fence_operands();
             arrive(&sh.q_full[t]);
         }
-        // last key that the row sees; keys in front of all_hi and from all_lo on are seen by every row of the tile
-        const int64_t last_row = (int64_t)s.tile * ROWS + t * TILE + TILE < all ? (int64_t)s.tile * ROWS + t * TILE + TILE - 1 : all - 1;
-        const int64_t hi = s.pos + (mine ? r : all - 1) / a.group;
-        const int64_t all_hi = s.pos + ((int64_t)s.tile * ROWS + t * TILE) / a.group + 1;
-        const int64_t all_lo = a.window > 0 ? s.pos + last_row / a.group - a.window + 1 : 0;
+        // last key that the row sees; keys in front of all_hi and from all_lo on are seen by every row of the tile (a key's position
+        // fits 32 bits; past the end of the range nothing is seen)
+        const int row0 = s.tile * ROWS + t * TILE, last_row = row0 + TILE <= all ? row0 + TILE - 1 : all - 1;
+        const int hi = (int)min((int64_t)s.pos + (mine ? r : all - 1) / a.group, (int64_t)0x7FFFFFFF);
+        const int all_hi = (int)min((int64_t)s.pos + row0 / a.group, (int64_t)0x7FFFFFFE) + 1;
+        const int all_lo = a.window > 0 ? (int)min((int64_t)s.pos + last_row / a.group - a.window, (int64_t)0x7FFFFFFE) + 1 : 0;
         float m = M_NONE, l = 0.f;
         int E = -1000;                                           // O holds sums of p * v * 2^(P_SHIFT - E)
         for (int u = s.u0; u < s.u1; ++u, ++g) {
@@ -553,7 +562,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
             const int ve = sh.ve[st];
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
-                const int64_t t0 = ((int64_t)s.s0 + 8 * u) * QP_KV_SLICE + h * HALF;
+                const int t0 = (s.s0 + 8 * u) * QP_KV_SLICE + h * HALF;
                 wait(sh, &sh.s_full[t][h], g & 1, a.wait_cycles);
                 __syncwarp();
                 fence_after();
@@ -565,7 +574,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
                 if ((valid[0] & valid[1]) != 0xFFFFFFFFu || t0 < all_lo || t0 + HALF > all_hi) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int64_t up = hi - t0 - 32 * c, down = a.window > 0 ? hi - a.window - t0 - 32 * c : -1;   // keys (down, up]
+                        const int up = hi - t0 - 32 * c, down = a.window > 0 ? hi - a.window - t0 - 32 * c : -1;   // keys (down, up]
                         unsigned seen = valid[c];
                         seen &= up < 0 ? 0u : up >= 31 ? 0xFFFFFFFFu : (2u << up) - 1u;
                         seen &= down < 0 ? 0xFFFFFFFFu : down >= 31 ? 0u : ~((2u << down) - 1u);
@@ -670,34 +679,46 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
             if (__all_sync(0xFFFFFFFFu, sh.last[t] != 0 && !given_up(sh))) {
                 __threadfence();
                 auto at = [&](int p) { return a.part + ((int64_t)(p ? 2 * (s.c0 + p) : s.first_at) * 2 + t) * C::PART; };
-                const int warp_row = row & ~31;
-                for (int k = 0; k < 32; ++k) {                   // a warp to a row
-                    const int64_t rr = (int64_t)s.tile * ROWS + t * TILE + warp_row + k;
-                    if (rr >= all) break;
-                    const int w = warp_row + k;
-                    float best = M_NONE;
-                    bool nan = false;
-                    for (int p = lane; p < parts; p += 32) {
-                        const float y = __ldcg(at(p) + TILE * D + w);
-                        nan |= !(y == y);
-                        best = fmaxf(best, y);
-                    }
+                const int warp_row = row & ~31, base_row = s.tile * ROWS + t * TILE;
+                // a lane's row: the parts' weights, and the sum of their sums
+                float best = M_NONE, sl = 0.f;
+                bool nan = false;
+                for (int p = 0; p < parts; ++p) {
+                    const float y = __ldcg(at(p) + TILE * D + row);
+                    nan |= !(y == y);
+                    best = fmaxf(best, y);
+                }
+                for (int p = 0; p < parts; ++p) {
+                    const float* x = at(p) + TILE * D + row;
+                    sl = fmaf(ex2(__ldcg(x) - best), __ldcg(x + TILE), sl);
+                }
+                // then 16 rows at a time, four elements to a lane
+                constexpr int LANES = D / 4, AT_ONCE = 16, STEP = 32 / LANES;
+#pragma unroll 1
+                for (int k0 = 0; k0 < 32; k0 += AT_ONCE * STEP) {
+                    float4 so[AT_ONCE];
 #pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) best = fmaxf(best, __shfl_xor_sync(0xFFFFFFFFu, best, o));
-                    nan = __any_sync(0xFFFFFFFFu, nan);
-                    float sl = 0.f;
-                    float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
+                    for (int k = 0; k < AT_ONCE; ++k) so[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    const int mine0 = warp_row + k0 + lane / LANES, d = 4 * (lane % LANES);
                     for (int p = 0; p < parts; ++p) {
                         const float* x = at(p);
-                        const float wt = ex2(__ldcg(x + TILE * D + w) - best);
-                        sl = fmaf(wt, __ldcg(x + TILE * D + TILE + w), sl);
-                        if (lane < D / 4) {
-                            const float4 y = __ldcg(reinterpret_cast<const float4*>(x + w * D) + lane);
-                            so.x = fmaf(wt, y.x, so.x); so.y = fmaf(wt, y.y, so.y); so.z = fmaf(wt, y.z, so.z); so.w = fmaf(wt, y.w, so.w);
+                        const float wt = ex2(__ldcg(x + TILE * D + row) - best);
+#pragma unroll
+                        for (int k = 0; k < AT_ONCE; ++k) {
+                            const int w = mine0 + k * STEP;
+                            const float4 y = base_row + w < all ? __ldcg(reinterpret_cast<const float4*>(x + w * D + d)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                            const float f = __shfl_sync(0xFFFFFFFFu, wt, w & 31);
+                            so[k].x = fmaf(f, y.x, so[k].x); so[k].y = fmaf(f, y.y, so[k].y);
+                            so[k].z = fmaf(f, y.z, so[k].z); so[k].w = fmaf(f, y.w, so[k].w);
                         }
                     }
-                    if (lane < D / 4) put_row<D>(a, s, rr, 4 * lane, so, best, sl, nan);
+#pragma unroll
+                    for (int k = 0; k < AT_ONCE; ++k) {
+                        const int w = mine0 + k * STEP;
+                        const float fm = __shfl_sync(0xFFFFFFFFu, best, w & 31), fl = __shfl_sync(0xFFFFFFFFu, sl, w & 31);
+                        const int fn = __shfl_sync(0xFFFFFFFFu, (int)nan, w & 31);
+                        if (base_row + w < all) put_row<D>(a, s, base_row + w, d, so[k], fm, fl, fn != 0);
+                    }
                 }
             }
         }
@@ -737,12 +758,12 @@ __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_a
 
     if (threadIdx.x == 0) {
         for (int t = 0; t < 2; ++t) {
-            qp_stream::mbar_init(&sh.q_full[t], TILE);
-            qp_stream::mbar_init(&sh.kv_full[t], 128);
+            qp_stream::mbar_init(&sh.q_full[t], 4);
+            qp_stream::mbar_init(&sh.kv_full[t], 4);
             qp_stream::mbar_init(&sh.kv_empty[t], 1);
             for (int h = 0; h < 2; ++h) {
                 qp_stream::mbar_init(&sh.s_full[t][h], 1);
-                qp_stream::mbar_init(&sh.p_full[t][h], TILE);
+                qp_stream::mbar_init(&sh.p_full[t][h], 4);
                 qp_stream::mbar_init(&sh.pv_done[t][h], 1);
             }
         }
@@ -780,23 +801,23 @@ __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_a
     __syncthreads();
     fence_after();
 
-    // Registers by role: 2 * 128 * 128 + 128 * 160 + 128 * 96 are the block's 512 * 128.  (A loop for each role, so that each
+    // Registers by role: 2 * 128 * 160 + 128 * 128 + 128 * 64 are the block's 512 * 128.  (A loop for each role, so that each
     // is compiled for its own number.)
     int g = 0;
     if (warp < 8) {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
         do {
             if (warp == 0) list_parts(a, sh, u, end, begin, W, blocks, b, base);
             block_sync();
             softmax<D>(a, sh, smem, g);
         } while (more_parts(sh));
     } else if (warp < 12) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 160;");
         do {
             block_sync();
             produce<D>(a, sh, stages, g);
         } while (more_parts(sh));
     } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
         int items = 0;
         do {
             block_sync();
