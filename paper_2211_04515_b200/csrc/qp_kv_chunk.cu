@@ -172,9 +172,10 @@ struct Shared {
     uint64_t q_full[2], kv_full[2], kv_empty[2], s_full[2][2], p_full[2][2], pv_done[2][2], all_done;
     uint32_t tmem, give_up;
     int n_segs, more;
-    float kinv[2];                               // per stage: what takes K's scaled values back
-    int ve[2];                                   // the power of two that V's were divided by
-    uint32_t valid[2][4];                        // keys that are there
+    // per stage: what takes K's scaled values back (bits of a float), the power of two that V's were divided by, and per 32 keys which
+    // are there
+    int2 about[2];
+    uint4 valid[2];
     float2 quant[2][2][TILE];                    // K's and V's quantizers of a tile
     float amax[2][2][4];
     int last[2];
@@ -269,9 +270,8 @@ __device__ __forceinline__ void list_parts(const qp_kv_attn_args& a, Shared& sh,
 // A wait with a limit.  Once one has run out none waits any more: every role goes on to the end of its loops, so that no barrier is
 // left with a part of its threads, and nothing more is written out.
 __device__ __forceinline__ bool given_up(const Shared& sh) { return *(const volatile uint32_t*)&sh.give_up != 0u; }
-__device__ __forceinline__ void wait(Shared& sh, uint64_t* bar, unsigned parity, long long limit)
+__device__ __forceinline__ void wait_on(Shared& sh, uint64_t* bar, unsigned parity, long long limit)
 {
-    if (qp_stream::mbar_try_wait(bar, parity)) return;
     const long long since = clock64();
     while (!qp_stream::mbar_try_wait(bar, parity)) {
         if (given_up(sh)) return;
@@ -280,6 +280,10 @@ __device__ __forceinline__ void wait(Shared& sh, uint64_t* bar, unsigned parity,
             return;
         }
     }
+}
+__device__ __forceinline__ void wait(Shared& sh, uint64_t* bar, unsigned parity, long long limit)
+{
+    if (!qp_stream::mbar_try_wait(bar, parity)) wait_on(sh, bar, parity, limit);
 }
 
 // ---------------------------------------------------------------------------- the cache's codes into operands
@@ -298,7 +302,7 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
         const Seg& s = sh.segs[i];
         const int held = s.pos + s.n, units = s.u1 - s.u0;
         // what a tile needs from memory, in registers: asked for one tile ahead, its places two
-        struct Raw { uint4 k[L], v[L]; float4 quant; unsigned there; } raw[2];
+        struct Raw { uint4 k[L], v[L]; float4 quant; unsigned there; } now, next;
         int64_t place = -1;
         auto look_up = [&](int u) {                              // lane i < 8 of each warp: slice i
             const int sl = s.s0 + 8 * u + lane, pg = sl / a.slices;
@@ -327,7 +331,7 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
             }
             x.there = __ballot_sync(0xFFFFFFFFu, there);
         };
-        auto convert = [&](const Raw& x) {
+        auto convert = [&](Raw& x) {
             const int st = g & 1;
             const float4 quant = x.quant;
             // powers of two for the tile
@@ -350,8 +354,8 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
             if (g >= 2) wait(sh, &sh.kv_empty[st], ((g >> 1) + 1) & 1, a.wait_cycles);
             __syncwarp();
             char* to = stages + st * (2 * C::OPERAND);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {                        // K, then V
                 const float f = h ? vf : kf;
 #pragma unroll
                 for (int l = 0; l < L; ++l) {
@@ -360,7 +364,7 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
                     // a nibble under 128's (or 2048's) exponent is 128 + code: lo + scale * code in one fused operation
                     const float sc = q.y * f, lo = q.x * f;
                     const qp_f2 s2 = qp_pack2(sc, sc), c2 = qp_pack2(fmaf(-128.f, sc, lo), fmaf(-2048.f, sc, lo));
-                    const uint4 codes = h ? x.v[l] : x.k[l];
+                    const uint4 codes = x.k[l];
                     const unsigned w4[4] = {codes.x, codes.y, codes.z, codes.w};
                     char* panel = to + h * C::OPERAND + (D == 128 ? (piece >> 1) * (TILE * 128) : 0) + key * 128;
                     const int c0 = D == 128 ? 4 * (piece & 1) : 4 * piece;
@@ -377,25 +381,24 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
                         *reinterpret_cast<uint4*>(panel + (((c0 + w) ^ (key & 7)) << 4)) = out;
                     }
                 }
+#pragma unroll
+                for (int l = 0; l < L; ++l) x.k[l] = x.v[l];
             }
-            if (p == 0) { sh.kinv[st] = pow2(ke); sh.ve[st] = ve; }
-            if (lane == 0) sh.valid[st][p >> 5] = x.there;
+            if (p == 0) sh.about[st] = make_int2(__float_as_int(pow2(ke)), ve);
+            if (lane == 0) (&sh.valid[st].x)[p >> 5] = x.there;
             fence_operands();
             arrive(&sh.kv_full[st]);
             ++g;
         };
         look_up(s.u0);
-        load(raw[0], s.u0);
+        load(now, s.u0);
         look_up(s.u0 + 1);
-        for (int u = 0; u < units; u += 2) {
-            load(raw[1], s.u0 + u + 1);                          // (behind the last: nothing)
+#pragma unroll 1
+        for (int u = 0; u < units; ++u) {
+            load(next, s.u0 + u + 1);                            // (behind the last: nothing)
             look_up(s.u0 + u + 2);
-            convert(raw[0]);
-            if (u + 1 < units) {
-                load(raw[0], s.u0 + u + 2);
-                look_up(s.u0 + u + 3);
-                convert(raw[1]);
-            }
+            convert(now);
+            now = next;
         }
     }
 }
@@ -411,73 +414,72 @@ __device__ __forceinline__ void multiply(const qp_kv_attn_args& a, Shared& sh, c
     // descriptors move on by 16-byte units of the address
     const uint64_t q_desc = operand_at(smem_of(q_at), 16), k_desc = operand_at(smem_of(stages), 16),
                    v_desc = operand_at(smem_of(stages) + C::OPERAND, TILE * 128);
-    // query tile t against half h of the key tile in stage st
-    auto scores = [&](int t, int st, int h) {
-        const uint64_t q = q_desc + (uint32_t)(t * (C::OPERAND / 16)), k = k_desc + (uint32_t)(st * (2 * C::OPERAND / 16) + h * (HALF * 128 / 16));
-        const uint32_t to = tm + t * TILE + h * HALF;
-#pragma unroll
-        for (int s = 0; s < D / 16; ++s) {
-            const uint32_t in = (uint32_t)(s >> 2) * (TILE * 128 / 16) + (uint32_t)(s & 3) * 2;
-            mma_ss(to, q + in, k + in, S_SHAPE, s > 0);
-        }
-        commit(&sh.s_full[t][h]);
-    };
     for (int i = 0; i < sh.n_segs; ++i, ++items) {
-        const int units = sh.segs[i].u1 - sh.segs[i].u0;
-        wait(sh, &sh.kv_full[g & 1], (g >> 1) & 1, a.wait_cycles);
-        for (int t = 0; t < 2; ++t) {
-            wait(sh, &sh.q_full[t], items & 1, a.wait_cycles);
-            fence_after();
-            scores(t, g & 1, 0);
-        }
-        for (int t = 0; t < 2; ++t) scores(t, g & 1, 1);
-        for (int u = 0; u < units; ++u, ++g) {
-            const int st = g & 1;
+        const int halves = 2 * (sh.segs[i].u1 - sh.segs[i].u0);
+        // weights of half k, then scores of half k + 2 in their place; each stands once in the code, which all roles share a cache for
 #pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
+        for (int k = -2; k < halves; ++k) {
+            const int h = k & 1, now = g + (k >> 1), st = now & 1;       // (k = -2, -1: tile g - 1, which there is none of)
+            if (k >= 0) {
+#pragma unroll 1
                 for (int t = 0; t < 2; ++t) {
-                    wait(sh, &sh.p_full[t][h], g & 1, a.wait_cycles);
+                    wait(sh, &sh.p_full[t][h], now & 1, a.wait_cycles);
                     fence_after();
                     const uint64_t v = v_desc + (uint32_t)(st * (2 * C::OPERAND / 16) + h * (HALF * 128 / 16));
                     const uint32_t to = tm + 2 * TILE + t * TILE, from = tm + t * TILE + h * HALF;
-                    const bool add = u > 0 || h > 0;
 #pragma unroll
-                    for (int s = 0; s < HALF / 16; ++s) mma_ts(to, from + s * 8, v + (uint32_t)(s * (2048 / 16)), O_SHAPE, add || s > 0);
+                    for (int s = 0; s < HALF / 16; ++s) mma_ts(to, from + s * 8, v + (uint32_t)(s * (2048 / 16)), O_SHAPE, k > 0 || s > 0);
                     commit(&sh.pv_done[t][h]);
                 }
                 if (h == 1) commit(&sh.kv_empty[st]);
-                if (u + 1 < units) {                             // the next tile's scores take the place of the weights just used
-                    if (h == 0) wait(sh, &sh.kv_full[st ^ 1], ((g + 1) >> 1) & 1, a.wait_cycles);
-                    for (int t = 0; t < 2; ++t) {
-                        wait(sh, &sh.pv_done[t][h], g & 1, a.wait_cycles);
-                        fence_after();
-                        scores(t, st ^ 1, h);
+            }
+            if (k + 2 < halves) {
+                if (h == 0) wait(sh, &sh.kv_full[st ^ 1], ((now + 1) >> 1) & 1, a.wait_cycles);
+#pragma unroll 1
+                for (int t = 0; t < 2; ++t) {
+                    if (k == -2) wait(sh, &sh.q_full[t], items & 1, a.wait_cycles);
+                    if (k >= 0) wait(sh, &sh.pv_done[t][h], now & 1, a.wait_cycles);
+                    fence_after();
+                    const uint64_t q = q_desc + (uint32_t)(t * (C::OPERAND / 16)), kk = k_desc + (uint32_t)((st ^ 1) * (2 * C::OPERAND / 16) + h * (HALF * 128 / 16));
+                    const uint32_t to = tm + t * TILE + h * HALF;
+#pragma unroll
+                    for (int s = 0; s < D / 16; ++s) {
+                        const uint32_t in = (uint32_t)(s >> 2) * (TILE * 128 / 16) + (uint32_t)(s & 3) * 2;
+                        mma_ss(to, q + in, kk + in, S_SHAPE, s > 0);
                     }
+                    commit(&sh.s_full[t][h]);
                 }
             }
         }
+        g += halves / 2;
     }
 }
 
 // ---------------------------------------------------------------------------- softmax
 
-// this row's out and lse
-template <int D>
-__device__ __forceinline__ void put_row(const qp_kv_attn_args& a, const Seg& s, int r, int d, float4 o, float m, float l, bool bad)
+// N elements of a row of out
+template <int N>
+__device__ __forceinline__ void put_out(unsigned short* to, bool vec, const float* v, float f, bool bad)
 {
-    const int64_t token = s.row0 + r / a.group;
-    const int h = s.head * a.group + r % a.group;
-    const float nan = __int_as_float(0x7FC00000);
-    float v[4] = {o.x, o.y, o.z, o.w};
-    unsigned short x[4];
-    unsigned short* to = static_cast<unsigned short*>(a.out) + token * a.ot + (int64_t)h * a.oh + d;
+    unsigned w[N / 2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = qp_f32_to_bf16(bad ? nan : l == 0.f ? 0.f : v[i] / l);
-    if (a.out_vec) *reinterpret_cast<uint2*>(to) = make_uint2(x[0] | ((unsigned)x[1] << 16), x[2] | ((unsigned)x[3] << 16));
-    else
+    for (int i = 0; i < N / 2; ++i) {
+        const float x = bad ? __int_as_float(0x7FC00000) : v[2 * i] * f, y = bad ? __int_as_float(0x7FC00000) : v[2 * i + 1] * f;
+        w[i] = qp_f32_to_bf16(x) | ((unsigned)qp_f32_to_bf16(y) << 16);
+    }
+    if (vec) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[i] = x[i];
-    if (a.lse && d == 0) a.lse[token * a.q_heads + h] = bad ? nan : l == 0.f ? -__int_as_float(0x7F800000) : (m + log2f(l)) * 0.6931471805599453f;
+        for (int i = 0; i < N / 4; ++i) *reinterpret_cast<uint2*>(to + 4 * i) = make_uint2(w[2 * i], w[2 * i + 1]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) { to[2 * i] = (unsigned short)w[i]; to[2 * i + 1] = (unsigned short)(w[i] >> 16); }
+    }
+}
+__device__ __forceinline__ void put_lse(const qp_kv_attn_args& a, int token, int head, float m, float l, bool bad)
+{
+    if (a.lse)
+        a.lse[(int64_t)token * a.q_heads + head] =
+            bad ? __int_as_float(0x7FC00000) : l == 0.f ? -__int_as_float(0x7F800000) : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 template <int D>
@@ -555,27 +557,30 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         const int all_lo = a.window > 0 ? (int)min((int64_t)s.pos + last_row / a.group - a.window, (int64_t)0x7FFFFFFE) + 1 : 0;
         float m = M_NONE, l = 0.f;
         int E = -1000;                                           // O holds sums of p * v * 2^(P_SHIFT - E)
-        for (int u = s.u0; u < s.u1; ++u, ++g) {
+        const int first_key = s.s0 * QP_KV_SLICE, u0 = s.u0, u1 = s.u1;
+        for (int u = u0; u < u1; ++u, ++g) {
             const int st = g & 1;
             wait(sh, &sh.kv_full[st], (g >> 1) & 1, a.wait_cycles);      // (long there: for what the producers say of the tile)
-            const float f = fmaxf(kf * sh.kinv[st], 1e-37f);     // (positive, so that -inf stays)
-            const int ve = sh.ve[st];
+            const int2 about = sh.about[st];
+            const uint4 v4 = sh.valid[st];
+            const float f = fmaxf(kf * __int_as_float(about.x), 1e-37f);         // (positive, so that -inf stays)
+            const int ve = about.y, key0 = first_key + u * TILE;
+            const bool whole = (v4.x & v4.y & v4.z & v4.w) == 0xFFFFFFFFu && key0 >= all_lo && key0 + TILE <= all_hi;
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
-                const int t0 = (s.s0 + 8 * u) * QP_KV_SLICE + h * HALF;
+                const int t0 = key0 + h * HALF;
                 wait(sh, &sh.s_full[t][h], g & 1, a.wait_cycles);
                 __syncwarp();
                 fence_after();
                 float x[HALF];
                 tmem_ld32(s_at + h * HALF, x);
                 tmem_ld32(s_at + h * HALF + 32, x + 32);
-                const unsigned valid[2] = {sh.valid[st][2 * h], sh.valid[st][2 * h + 1]};
                 wait_ld(x);
-                if ((valid[0] & valid[1]) != 0xFFFFFFFFu || t0 < all_lo || t0 + HALF > all_hi) {
+                if (!whole) {
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
                         const int up = hi - t0 - 32 * c, down = a.window > 0 ? hi - a.window - t0 - 32 * c : -1;   // keys (down, up]
-                        unsigned seen = valid[c];
+                        unsigned seen = h ? (c ? v4.w : v4.z) : (c ? v4.y : v4.x);
                         seen &= up < 0 ? 0u : up >= 31 ? 0xFFFFFFFFu : (2u << up) - 1u;
                         seen &= down < 0 ? 0xFFFFFFFFu : down >= 31 ? 0u : ~((2u << down) - 1u);
 #pragma unroll
@@ -597,7 +602,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
                         back *= E < -999 ? 0.f : pow2(E - ve);
                         E = ve;
                     }
-                    if (u > s.u0 || h > 0) {
+                    if (u > u0 || h > 0) {
                         wait(sh, &sh.pv_done[t][h ^ 1], (h ? g : g - 1) & 1, a.wait_cycles);      // of the half before
                         __syncwarp();
                         fence_after();
@@ -646,8 +651,10 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         __syncwarp();
         fence_after();
         const bool out = mine && !given_up(sh);
-        const float un = pow2(E - P_SHIFT);
         float* part = a.part + ((int64_t)s.at * 2 + t) * C::PART;
+        const int token = s.row0 + r / a.group, head = s.head * a.group + r % a.group;      // (of a row that is there)
+        unsigned short* to = static_cast<unsigned short*>(a.out) + (int64_t)token * a.ot + (int64_t)head * a.oh;
+        const float un = pow2(E - P_SHIFT), over = s.split ? 1.f : l == 0.f ? 0.f : 1.f / l;
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
             float y[32];
@@ -655,13 +662,14 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
             wait_ld(y);
             if (out) {
 #pragma unroll
-                for (int e = 0; e < 32; e += 4) {
-                    const float4 o = make_float4(y[e] * un, y[e + 1] * un, y[e + 2] * un, y[e + 3] * un);
-                    if (!s.split) put_row<D>(a, s, r, 32 * c + e, o, m, l, bad);
-                    else __stcg(reinterpret_cast<float4*>(part + row * D + 32 * c + e), o);
-                }
+                for (int e = 0; e < 32; ++e) y[e] *= un;
+                if (!s.split) put_out<32>(to + 32 * c, a.out_vec, y, over, bad);
+                else
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) __stcg(reinterpret_cast<float4*>(part + row * D + 32 * c + e), make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]));
             }
         }
+        if (out && !s.split) put_lse(a, token, head, m, l, bad);
         if (s.split) {
             if (out) {
                 __stcg(part + TILE * D + row, bad ? __int_as_float(0x7FC00000) : m);
@@ -715,11 +723,14 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
 #pragma unroll
                     for (int k = 0; k < AT_ONCE; ++k) {
                         const int w = mine0 + k * STEP;
-                        const float fm = __shfl_sync(0xFFFFFFFFu, best, w & 31), fl = __shfl_sync(0xFFFFFFFFu, sl, w & 31);
+                        const float f = __shfl_sync(0xFFFFFFFFu, sl == 0.f ? 0.f : 1.f / sl, w & 31);
                         const int fn = __shfl_sync(0xFFFFFFFFu, (int)nan, w & 31);
-                        if (base_row + w < all) put_row<D>(a, s, base_row + w, d, so[k], fm, fl, fn != 0);
+                        const int64_t at_row = __shfl_sync(0xFFFFFFFFu, (int64_t)token * a.ot + (int64_t)head * a.oh, w & 31);
+                        const float y[4] = {so[k].x, so[k].y, so[k].z, so[k].w};
+                        if (base_row + w < all) put_out<4>(static_cast<unsigned short*>(a.out) + at_row + d, a.out_vec, y, f, fn != 0);
                     }
                 }
+                if (mine) put_lse(a, token, head, best, sl, nan);
             }
         }
         fence_before();
@@ -768,7 +779,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_a
             }
         }
         qp_stream::mbar_init(&sh.all_done, 1);
-        sh.give_up = 0u;
+        sh.give_up = a.wait_cycles <= 0 ? 1u : 0u;               // (a limit of nothing has run out: test only)
         qp_stream::fence_barrier_init();
     }
     if (warp == 12) {
