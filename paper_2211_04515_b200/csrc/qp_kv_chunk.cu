@@ -12,10 +12,13 @@
 // What bounds it: 4 * 256 * 128 * D operations of the products (2048 cycles at D = 128 and the nominal rate) and as many cycles for
 // the 32768 exponentials (16 a cycle).  So a softmax element gets three more operations and no more: the codes are not multiplied
 // as they are, as for few queries (their quantizers would cost two operations and shared-memory reads on every score and weight), but
-// as lo + scale * code, put together in fp32 and rounded once to fp16.  That costs 20 operations to 8 codes, a third of
-// the softmax's for 256 rows.  The rounding is 2^-11 of a value at most, an eighth of what the rounding of K to bf16 would be.  fp16's
-// range: each tile of K and of V is scaled by a power of two that takes its largest value to [2^10, 2^11); queries are scaled by
-// row.  K's power goes into the factor of the scores, V's into the exponent of the weights (both are one number a tile).
+// as their values in fp16: a nibble under 1024's exponent is 1024 + code (or + 16 * code), less 1032 it is code - 8, and a fused
+// operation takes two of them to (lo + 8 scale) + scale * (code - 8): 13 operations to 8 codes.  (In fp32 first, rounded once: 20, and the whole
+// kernel 14 % slower.  The nibbles as subnormals, without the subtraction: 10, but the range left for values is 2^20 within a tile.)
+// The result, scale and the value of code 8 are each rounded to 11 bits, an eighth of what bf16 would lose.  (About code 0 instead: lo is
+// several times the middle of a row, and its rounding moves a whole row of scores; the result was 1.6 times as far off.)  fp16's range: each tile of K and of V is scaled by a power of two that takes its largest
+// value to [2^10, 2^11); queries are scaled by row.  K's power goes into the factor of the scores, V's into the exponent of
+// the weights (both are one number a tile).  Elements lie in the order 0 4 1 5 2 6 3 7 of each eight, in the operands and in O.
 //
 //   - Softmax reference raised only when a score passes it by 8 (log2): then O is read from tensor memory, scaled and put back.
 //   - The work, in key tiles, is cut into equal runs for the SMs; an item that a cut falls into leaves partial results
@@ -143,11 +146,25 @@ __device__ __forceinline__ unsigned half2_of(float lo, float hi)
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ unsigned half2_of(qp_f2 v)
+__device__ __forceinline__ unsigned mul_h2(unsigned a, unsigned b)
 {
-    float a, b;
-    qp_unpack2(v, a, b);
-    return half2_of(a, b);
+    unsigned r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ unsigned fma_h2(unsigned a, unsigned b, unsigned c)
+{
+    unsigned r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+// codes less 8 (16 times that under the higher mask): 1024 + x has x in its low bits
+template <unsigned MASK>
+__device__ __forceinline__ unsigned nibbles(unsigned w)
+{
+    unsigned r = (w & MASK) | 0x64006400u;
+    asm("sub.f16x2 %0, %0, %1;" : "+r"(r) : "r"(MASK == 0x000F000Fu ? 0x64086408u : 0x64806480u));
+    return r;
 }
 // a warp's arrival, for all that its lanes did before
 __device__ __forceinline__ void arrive(uint64_t* bar)
@@ -361,23 +378,19 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
                 for (int l = 0; l < L; ++l) {
                     const int sl = (l * 128 + p) / PER, key = sl * QP_KV_SLICE + row;
                     const float2 q = sh.quant[st][h][key];
-                    // a nibble under 128's (or 2048's) exponent is 128 + code: lo + scale * code in one fused operation
-                    const float sc = q.y * f, lo = q.x * f;
-                    const qp_f2 s2 = qp_pack2(sc, sc), c2 = qp_pack2(fmaf(-128.f, sc, lo), fmaf(-2048.f, sc, lo));
+                    const float sc = q.y * f;
+                    const unsigned m1 = half2_of(sc, sc), m16 = mul_h2(m1, 0x2C002C00u);         // (times 2^-4)
+                    const float mid = fmaf(8.f, sc, q.x * f);
+                    const unsigned base = half2_of(mid, mid);
                     const uint4 codes = x.k[l];
                     const unsigned w4[4] = {codes.x, codes.y, codes.z, codes.w};
                     char* panel = to + h * C::OPERAND + (D == 128 ? (piece >> 1) * (TILE * 128) : 0) + key * 128;
                     const int c0 = D == 128 ? 4 * (piece & 1) : 4 * piece;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        const unsigned even[4] = {w4[w] << 16, w4[w] << 8, w4[w], w4[w] >> 8};   // bits 16..19: codes 0, 2, 4, 6
-                        const unsigned odd[4] = {w4[w] << 8, w4[w], w4[w] >> 8, w4[w] >> 16};    // bits 12..15: codes 1, 3, 5, 7
-                        uint4 out;
-                        unsigned* o = &out.x;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            o[e] = half2_of(qp_fma2(qp_pack2(__uint_as_float((even[e] & 0x000F0000u) | 0x43000000u),
-                                                             __uint_as_float((odd[e] & 0x0000F000u) | 0x45000000u)), s2, c2));
+                        const unsigned high = w4[w] >> 8;        // codes 0 4, 1 5 and 2 6, 3 7 at bits 0..3, 4..7 of each half
+                        const uint4 out = make_uint4(fma_h2(nibbles<0x000F000Fu>(w4[w]), m1, base), fma_h2(nibbles<0x00F000F0u>(w4[w]), m16, base),
+                                                     fma_h2(nibbles<0x000F000Fu>(high), m1, base), fma_h2(nibbles<0x00F000F0u>(high), m16, base));
                         *reinterpret_cast<uint4*>(panel + (((c0 + w) ^ (key & 7)) << 4)) = out;
                     }
                 }
@@ -540,8 +553,9 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
                 const unsigned w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
                 unsigned h[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float y0 = __uint_as_float(w[e] << 16), y1 = __uint_as_float(w[e] & 0xFFFF0000u);
+                for (int e = 0; e < 4; ++e) {                    // elements e and e + 4
+                    const float y0 = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+                    const float y1 = __uint_as_float(e & 1 ? w[e / 2 + 2] & 0xFFFF0000u : w[e / 2 + 2] << 16);
                     h[e] = bad ? 0u : half2_of(y0 * norm, y1 * norm);
                 }
                 *reinterpret_cast<uint4*>(to + (c >> 3) * (TILE * 128) + (((c & 7) ^ (row & 7)) << 4)) = make_uint4(h[0], h[1], h[2], h[3]);
@@ -663,10 +677,13 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
             if (out) {
 #pragma unroll
                 for (int e = 0; e < 32; ++e) y[e] *= un;
-                if (!s.split) put_out<32>(to + 32 * c, a.out_vec, y, over, bad);
+                float z[32];                                     // in the elements' own order
+#pragma unroll
+                for (int e = 0; e < 32; ++e) z[(e & ~7) + ((e & 7) >> 1) + 4 * (e & 1)] = y[e];
+                if (!s.split) put_out<32>(to + 32 * c, a.out_vec, z, over, bad);
                 else
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4) __stcg(reinterpret_cast<float4*>(part + row * D + 32 * c + e), make_float4(y[e], y[e + 1], y[e + 2], y[e + 3]));
+                    for (int e = 0; e < 32; e += 4) __stcg(reinterpret_cast<float4*>(part + row * D + 32 * c + e), make_float4(z[e], z[e + 1], z[e + 2], z[e + 3]));
             }
         }
         if (out && !s.split) put_lse(a, token, head, m, l, bad);

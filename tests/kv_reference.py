@@ -60,7 +60,7 @@ def attention_row(q, k, v, visible, scale, weight_eps, out_eps, halves=False):
     vv, vlo, vs, vc = v
     if not visible.any():
         return np.zeros(len(q)), -np.inf, np.zeros(len(q)), 0.0
-    kv, klo, ks, vv, vs, vc = kv[visible], klo[visible], ks[visible], vv[visible], vs[visible], vc[visible]
+    kv, klo, ks, vv, vlo, vs, vc = (x[visible] for x in (kv, klo, ks, vv, vlo, vs, vc))
     s = kv @ q * scale
     top = s.max()
     p = np.exp(s - top)
@@ -76,11 +76,14 @@ def attention_row(q, k, v, visible, scale, weight_eps, out_eps, halves=False):
     n = len(s)
     weights = weight_eps * (p * vs) @ vc / l + n * 15 * 2.0 ** -29 * vs.max() / l
     if halves:
-        # A row's value is rounded to fp16 (2^-11 of itself, or 2^-35 of its tile's largest) from a fused operation whose constant,
-        # lo - 2048 scale at most, is off by up to 2^-24 * 2048 scale; a weight p to fp16 too, or to 2^-30 of the values' power of two,
-        # which is below 2^-10 of their largest times 2^11.
-        ds += abs(scale) * (np.abs(kv) @ np.abs(q) * 2.0 ** -11 + np.abs(q).sum() * (2.0 ** -13 * ks + 2.0 ** -35 * np.abs(kv).max())).max()
-        weights = p @ (2.0 ** -10 * np.abs(vv) + (2.0 ** -13 * vs + 2.0 ** -35 * np.abs(vv).max())[:, None]) / l + n * 2.0 ** -28 * np.abs(vv).max() / l
+        # A row's value v = mid + scale (c - 8), mid = lo + 8 scale, is rounded to fp16 (2^-11 of itself), and so are mid (2^-11) and
+        # scale (2^-11, times at most 8); values are scaled to a tile's largest at 2^10 or above, so a subnormal's
+        # 2^-25 is 2^-35 of that largest, twice (mid and the result).  A weight p is rounded to fp16 too, or to 2^-25 / 2^5 of its
+        # value at the power of two of the largest values.
+        def rounding(x, lo, scale):
+            return 2.0 ** -11 * (np.abs(x) + (np.abs(lo + 8 * scale) + 8 * scale)[:, None]) + 2.0 ** -34 * np.abs(x).max()
+        ds += abs(scale) * (rounding(kv, klo, ks) @ np.abs(q)).max()
+        weights = p @ (rounding(vv, vlo, vs) + 2.0 ** -11 * np.abs(vv)) / l + n * 2.0 ** -28 * np.abs(vv).max() / l
     err = (2 * ds + 2.0 ** -20 + (n / 8 + 16) * 2.0 ** -24) * spread + weights
     return out, top + np.log(l), err + out_eps * (np.abs(out) + err), 2 * ds + (n / 8 + 16) * 2.0 ** -23 + 2.0 ** -20 * (1 + abs(top))
 
