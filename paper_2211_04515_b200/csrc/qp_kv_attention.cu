@@ -39,7 +39,7 @@ constexpr float M_NONE = -3.0e38f;               // reference before any score
 constexpr float M_SLACK = 8.f;                   // a score may pass the reference by this (log2)
 constexpr float V_SLACK = 64.f;                  // and a scale of V its norm by this: p * scale' <= 2^14 in fp16
 constexpr int UNIT = 4;                          // slices
-constexpr int HEAD = 3;                          // units
+constexpr int HEAD = 6;                          // units
 constexpr int MANY = 64;                         // query rows to a cached head from which on the tensor-memory kernel is the faster
 
 template <int D, int NT, bool SPLIT> struct Cfg {
@@ -141,6 +141,22 @@ struct Seq {
     int64_t work;                                // units in all
 };
 
+// what follows from pos, n, row0 and slot
+template <int ROWS>
+__device__ __forceinline__ void derive(const qp_kv_attn_args& a, Seq& q)
+{
+    if (q.n <= 0 || q.pos < 0 || (int64_t)q.n * a.group >= a.many) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return; }
+    const unsigned most = (unsigned)a.pages.max_pages * (unsigned)a.pages.page_size;     // (below 2^31, as pos and n)
+    const unsigned end0 = (unsigned)q.pos + (unsigned)q.n, end = end0 < most ? end0 : most;
+    unsigned lo = a.window > 0 && q.pos >= a.window ? (unsigned)(q.pos - a.window + 1) : 0u;
+    if (lo > end) lo = end;
+    q.s0 = (int)(lo / QP_KV_SLICE);
+    q.s1 = (int)((end + QP_KV_SLICE - 1) / QP_KV_SLICE);
+    q.units = (q.s1 - q.s0 + UNIT - 1) / UNIT;
+    q.units = (q.units < 1 ? 1 : q.units) + HEAD;                // (an empty one still writes its rows)
+    q.tiles = (int)(((unsigned)q.n * (unsigned)a.group + ROWS - 1) / ROWS);
+    q.work = (int64_t)q.units * q.tiles * a.heads;
+}
 template <int ROWS>
 __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
 {
@@ -151,18 +167,7 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
     const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
     q.n = row1 - q.row0;
     if (q.n > a.max_new) q.n = a.max_new;
-    if (q.n <= 0 || q.pos < 0 || (int64_t)q.n * a.group >= a.many) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return q; }
-    const int64_t most = (int64_t)a.pages.max_pages * a.pages.page_size;
-    int64_t end = (int64_t)q.pos + q.n;
-    if (end > most) end = most;
-    int lo = a.window > 0 && q.pos >= a.window ? q.pos - a.window + 1 : 0;
-    if (lo > end) lo = (int)end;
-    q.s0 = lo / QP_KV_SLICE;
-    q.s1 = (int)((end + QP_KV_SLICE - 1) / QP_KV_SLICE);
-    q.units = (q.s1 - q.s0 + UNIT - 1) / UNIT;
-    q.units = (q.units < 1 ? 1 : q.units) + HEAD;                // (an empty one still writes its rows)
-    q.tiles = (int)(((int64_t)q.n * a.group + ROWS - 1) / ROWS);
-    q.work = (int64_t)q.units * q.tiles * a.heads;
+    derive<ROWS>(a, q);
     return q;
 }
 
@@ -170,6 +175,7 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
 // up to the last.
 struct Chunk {
     int64_t before[THREADS + 1];
+    int4 seq[THREADS];                           // pos, n, row0, slot
     int64_t sum[WARPS];
     int found;
 };
@@ -177,8 +183,7 @@ template <int ROWS>
 __device__ __forceinline__ int64_t load_chunk(const qp_kv_attn_args& a, int b0, int64_t base, Chunk& sh)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = b0 + threadIdx.x;
-    Seq q;
-    q.work = 0;
+    Seq q = {-1, 0, 0, 0, 0, 0, 0, 0, 0};
     if (b < a.rows.batch) q = seq_of<ROWS>(a, b);
     int64_t x = q.work;
 #pragma unroll
@@ -188,6 +193,7 @@ __device__ __forceinline__ int64_t load_chunk(const qp_kv_attn_args& a, int b0, 
     }
     __syncthreads();                                             // nobody reads the chunk before this any more
     if (lane == 31) sh.sum[warp] = x;
+    sh.seq[threadIdx.x] = make_int4(q.pos, q.n, q.row0, q.slot);
     __syncthreads();
     int64_t front = base;
 #pragma unroll
@@ -264,16 +270,15 @@ __device__ __forceinline__ void put_row(const qp_kv_attn_args& a, const Seq& q, 
 // Whether this block is the last of n to come here (the counter is at zero again then).  What the others wrote before is visible.
 __device__ __forceinline__ bool arrived(unsigned* count, int n, int& sh)
 {
-    __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {
+        __threadfence();                                         // (for the whole block's writes: the barrier put them in front)
         sh = atomicAdd(count, 1u) == (unsigned)(n - 1);
         if (sh) *count = 0u;
+        __threadfence();
     }
     __syncthreads();
-    const bool last = sh != 0;
-    if (last) __threadfence();
-    return last;
+    return sh != 0;
 }
 
 // Adds n partial results: the first at place `at`, part i > 0 at place even + 2 * step * i; in that order.  Into `sum`, a partial
@@ -366,7 +371,12 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         __syncthreads();
         if (u >= chunk.before[threadIdx.x] && u < chunk.before[threadIdx.x + 1]) chunk.found = threadIdx.x;
         __syncthreads();
-        const Seq q = seq_of<ROWS>(a, b0 + chunk.found);
+        Seq q;
+        {
+            const int4 x = chunk.seq[chunk.found];
+            q.pos = x.x; q.n = x.y; q.row0 = x.z; q.slot = x.w;
+            derive<ROWS>(a, q);
+        }
         const int64_t front = chunk.before[chunk.found], local = u - front, item = quotient(local, q.units);
         const int g0 = (int)(local - item * q.units), g1 = (int)(q.units - g0 < end - u ? q.units : g0 + (end - u));
         const int64_t here = u;
@@ -394,7 +404,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         int put = 0, take = 0;                                   // places in the ring
         auto issue = [&](int i) {                                // the warp's slice number i
             if (i < count * SL) {
-                if ((i & 31) == 0) look_up(i >> 5);
+                if ((i & 31) == 0 && i > 0) look_up(i >> 5);
                 const int64_t from = __shfl_sync(0xFFFFFFFFu, place, i & 31);
                 if (lane == 0) sh_ok[warp][put] = from >= 0;
                 if (from >= 0) {
@@ -408,6 +418,20 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             }
             copies_close();
         };
+        // (the page numbers and the queries are asked for together, and the copies go out before the queries are looked at)
+        if (count > 0) look_up(0);
+        float e[NT][D / 4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int r = tile * ROWS + 8 * t + n;
+            if (8 * t + n < rows) {
+                const int token = q.row0 + r / a.group, h = head * a.group + r % a.group;
+                load_q(static_cast<const T*>(a.q) + (int64_t)token * a.qt + (int64_t)h * a.qh + j * (D / 4), a.vec, e[t]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < D / 4; ++i) e[t][i] = 0.f;
+            }
+        }
 #pragma unroll
         for (int i = 0; i < STAGES; ++i) issue(i);
 
@@ -417,19 +441,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         int hi[NT][2];                                           // last key that the column's query sees
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            float e[D / 4];
-            const int r = tile * ROWS + 8 * t + n;
-            const bool mine = 8 * t + n < rows;
-            if (mine) {
-                const int token = q.row0 + r / a.group, h = head * a.group + r % a.group;
-                load_q(static_cast<const T*>(a.q) + (int64_t)token * a.qt + (int64_t)h * a.qh + j * (D / 4), a.vec, e);
-            } else {
-#pragma unroll
-                for (int i = 0; i < D / 4; ++i) e[i] = 0.f;
-            }
             float top = 0.f, sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) { top = fmaxf(top, fabsf(e[i])); sum += e[i]; }
+            for (int i = 0; i < D / 4; ++i) { top = fmaxf(top, fabsf(e[t][i])); sum += e[t][i]; }
 #pragma unroll
             for (int o = 1; o < 4; o <<= 1) {
                 top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
@@ -441,10 +455,10 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             ex = top == 0.f ? 127 : ex > 254 ? 254 : ex;
             const float norm = __uint_as_float((unsigned)ex << 23);
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) e[i] = bad ? 0.f : e[i] * norm;
+            for (int i = 0; i < D / 4; ++i) e[t][i] = bad ? 0.f : e[t][i] * norm;
 #pragma unroll
             for (int w = 0; w < KW; ++w) {
-                const float* x = e + 8 * w;
+                const float* x = e[t] + 8 * w;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {                    // nibbles i and i + 4; odd ones stand a factor 16 higher
                     const float f = i & 1 ? 0.0625f : 1.f;
