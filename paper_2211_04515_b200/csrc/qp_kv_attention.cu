@@ -177,8 +177,44 @@ struct Chunk {
     int64_t before[THREADS + 1];
     int4 seq[THREADS];                           // pos, n, row0, slot
     int64_t sum[WARPS];
-    int found;
 };
+// A part of an item: the run of units that one block has of it.
+struct Part {
+    Seq q;
+    int64_t u, next;                             // first unit and the one behind the last, counted with the items' heads
+    int g0, u0, u1;                              // the first in the item, with its head; units without it
+    int head, tile, rows;
+};
+// The part that begins with unit u of the chunk in shared memory; a warp does this by itself.
+template <int ROWS>
+__device__ __forceinline__ void find_part(const qp_kv_attn_args& a, const Chunk& sh, int64_t u, int64_t end, Part& to)
+{
+    const int lane = threadIdx.x & 31;
+    unsigned hit = 0;
+    int at = 0;
+#pragma unroll
+    for (int k = 0; k < THREADS / 32; ++k) {
+        const unsigned in = __ballot_sync(0xFFFFFFFFu, u >= sh.before[32 * k + lane] && u < sh.before[32 * k + lane + 1]);
+        if (in) { hit = in; at = 32 * k; }
+    }
+    at += __ffs(hit) - 1;
+    const int4 x = sh.seq[at];
+    Part p;
+    p.q.pos = x.x; p.q.n = x.y; p.q.row0 = x.z; p.q.slot = x.w;
+    derive<ROWS>(a, p.q);
+    const int64_t local = u - sh.before[at], item = quotient(local, p.q.units);
+    p.g0 = (int)(local - item * p.q.units);
+    const int g1 = (int)(p.q.units - p.g0 < end - u ? p.q.units : p.g0 + (end - u));
+    p.u = u;
+    p.next = u + (g1 - p.g0);
+    p.u0 = p.g0 > HEAD ? p.g0 - HEAD : 0;
+    p.u1 = g1 - HEAD;
+    p.head = (int)quotient(item, p.q.tiles);
+    p.tile = (int)(item - (int64_t)p.head * p.q.tiles);
+    const int all = p.q.n * a.group - p.tile * ROWS;
+    p.rows = all < ROWS ? all : ROWS;
+    if (lane == 0) to = p;
+}
 template <int ROWS>
 __device__ __forceinline__ int64_t load_chunk(const qp_kv_attn_args& a, int b0, int64_t base, Chunk& sh)
 {
@@ -289,44 +325,59 @@ __device__ __forceinline__ void add_parts(const qp_kv_attn_args& a, const Seq& q
 {
     constexpr int PART = ROWS * (D + 2);
     auto part = [&](int i) { return a.part + (int64_t)(i ? even + 2 * step * i : at) * PART; };
-    float* f = reinterpret_cast<float*>(smem);                   // [n][ROWS] factors, then [ROWS] references and sums
-    float* tops = f + n * ROWS;
+    float* f = reinterpret_cast<float*>(smem);                   // [n][2 ROWS] references, then factors, and sums; [ROWS] of the whole
+    float* tops = f + n * 2 * ROWS;
     __syncthreads();                                             // shared memory is free
-    for (int i = threadIdx.x; i < n * rows; i += THREADS) {
-        const int p = i / rows, r = i - p * rows;
-        f[p * ROWS + r] = __ldcg(part(p) + ROWS * D + r);
-    }
+    for (int i = threadIdx.x; i < n * 2 * ROWS; i += THREADS) f[i] = __ldcg(part(i / (2 * ROWS)) + ROWS * D + i % (2 * ROWS));
     __syncthreads();
-    for (int r = threadIdx.x >> 5; r < rows; r += WARPS) {       // a warp to a row
-        const int lane = threadIdx.x & 31;
-        float top = M_NONE;
-        for (int p = lane; p < n; p += 32) top = fmaxf(top, f[p * ROWS + r]);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-        float l = 0.f;
-        for (int p = lane; p < n; p += 32) {
-            const float w = ex2(f[p * ROWS + r] - top);
-            f[p * ROWS + r] = w;
-            l = fmaf(w, __ldcg(part(p) + ROWS * D + ROWS + r), l);
-        }
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xFFFFFFFFu, l, o);
-        if (lane == 0) { tops[r] = top; tops[ROWS + r] = l; }
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
-        const int r = i / (D / 4), d = 4 * (i % (D / 4));
-        float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
+    if (threadIdx.x < (unsigned)rows) {
+        const int r = threadIdx.x;
+        float top = M_NONE, l = 0.f;
+        for (int p = 0; p < n; ++p) top = fmaxf(top, f[p * 2 * ROWS + r]);
         for (int p = 0; p < n; ++p) {
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(part(p) + r * D + d));
-            const float w = f[p * ROWS + r];
-            so.x = fmaf(y.x, w, so.x); so.y = fmaf(y.y, w, so.y); so.z = fmaf(y.z, w, so.z); so.w = fmaf(y.w, w, so.w);
+            const float w = ex2(f[p * 2 * ROWS + r] - top);
+            f[p * 2 * ROWS + r] = w;
+            l = fmaf(w, f[p * 2 * ROWS + ROWS + r], l);
         }
+        tops[r] = top;
+        tops[ROWS + r] = l;
+    }
+    __syncthreads();
+    // all of a thread's elements of some parts are asked for at once: what this costs is the trips to L2
+    constexpr int MINE = ROWS * (D / 4) / THREADS, AT_ONCE = 8 / MINE > 0 ? 8 / MINE : 1;
+    float4 so[MINE];
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) so[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int last = rows * (D / 4) - 1;
+#pragma unroll 1
+    for (int p0 = 0; p0 < n; p0 += AT_ONCE) {
+        float4 y[AT_ONCE][MINE];
+#pragma unroll
+        for (int p = 0; p < AT_ONCE; ++p)
+#pragma unroll
+            for (int k = 0; k < MINE; ++k) {                     // (past the end: again the last, with no weight)
+                const int i = threadIdx.x + k * THREADS;
+                y[p][k] = __ldcg(reinterpret_cast<const float4*>(part(p0 + p < n ? p0 + p : n - 1)) + (i < last ? i : last));
+            }
+#pragma unroll
+        for (int p = 0; p < AT_ONCE; ++p)
+#pragma unroll
+            for (int k = 0; k < MINE; ++k) {
+                const int i = threadIdx.x + k * THREADS;
+                const float w = p0 + p < n ? f[(p0 + p) * 2 * ROWS + (i < last ? i : last) / (D / 4)] : 0.f;
+                const float4 x = p0 + p < n ? y[p][k] : make_float4(0.f, 0.f, 0.f, 0.f);
+                so[k].x = fmaf(x.x, w, so[k].x); so[k].y = fmaf(x.y, w, so[k].y);
+                so[k].z = fmaf(x.z, w, so[k].z); so[k].w = fmaf(x.w, w, so[k].w);
+            }
+    }
+#pragma unroll
+    for (int k = 0; k < MINE; ++k) {
+        const int i = threadIdx.x + k * THREADS, r = i / (D / 4), d = 4 * (i % (D / 4));
+        if (r >= rows) continue;
         if (!sum) {
-            put_row<T, D>(a, q, head, tile * ROWS + r, d, so, tops[r], tops[ROWS + r]);
+            put_row<T, D>(a, q, head, tile * ROWS + r, d, so[k], tops[r], tops[ROWS + r]);
         } else {
-            __stcg(reinterpret_cast<float4*>(sum + r * D + d), so);
+            __stcg(reinterpret_cast<float4*>(sum + r * D + d), so[k]);
             if (d == 0) { __stcg(sum + ROWS * D + r, tops[r]); __stcg(sum + ROWS * D + ROWS + r, tops[ROWS + r]); }
         }
     }
@@ -344,7 +395,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     constexpr unsigned M0 = 0x000F000Fu, M1 = 0x00F000F0u;
     extern __shared__ __align__(16) char smem[];
     __shared__ Chunk chunk;
-    __shared__ int sh_ok[WARPS][STAGES];
+    __shared__ Part part[2];
+    __shared__ int sh_ok[WARPS][STAGES], sh_hi[WARPS][ROWS];    // slices that are there; last key that a query sees
     __shared__ int sh_last;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = lane >> 2, j = lane & 3;
 
@@ -366,45 +418,57 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     const int v0 = (2 * j) ^ (j & 1), v1 = (2 * j + 1) ^ (j & 1);   // the same for rows 2j and 2j + 1
     bool flag = false;
 
-    for (int64_t u = begin; u < end;) {
-        while (u >= upto) { base = upto; upto = load_chunk<ROWS>(a, b0 += THREADS, base, chunk); }
-        __syncthreads();
-        if (u >= chunk.before[threadIdx.x] && u < chunk.before[threadIdx.x + 1]) chunk.found = threadIdx.x;
-        __syncthreads();
-        Seq q;
-        {
-            const int4 x = chunk.seq[chunk.found];
-            q.pos = x.x; q.n = x.y; q.row0 = x.z; q.slot = x.w;
-            derive<ROWS>(a, q);
+    // Lane i: the warp's slice number 32 * k + i of a part, and where it lies (-1: nowhere) by the table's entry.  The first entries of
+    // a part are asked for while the one before it is finished.
+    auto slice_of = [&](const Part& p, int k) {
+        return p.q.s0 + UNIT * p.u0 + SL * warp + SL * WARPS * ((32 * k + lane) / SL) + (SL == 2 ? lane & 1 : 0);
+    };
+    auto stop_of = [&](const Part& p) { const int s = p.q.s0 + UNIT * p.u1; return s < p.q.s1 ? s : p.q.s1; };
+    auto ask = [&](const Part& p, int k) {
+        const int s = slice_of(p, k), i = s / a.slices;
+        const bool in = s < stop_of(p) && (unsigned)p.q.slot < (unsigned)a.pages.max_seqs && i < a.pages.max_pages;
+        return in ? __ldg(a.pages.table + (size_t)p.q.slot * a.pages.max_pages + i) : -1;
+    };
+    auto place_of = [&](const Part& p, int k, int page) {
+        const int s = slice_of(p, k);
+        if (s >= stop_of(p)) return (int64_t)-1;
+        const bool in = page >= 0 && page < a.pages.num_pages;
+        flag |= !in;
+        return in ? (((int64_t)page * a.heads + p.head) * a.slices + s % a.slices) * SB : (int64_t)-1;
+    };
+
+    __syncthreads();
+    if (warp == 0) find_part<ROWS>(a, chunk, begin, end, part[0]);
+    __syncthreads();
+    int entry = ask(part[0], 0);
+    for (int turn = 0;; turn ^= 1) {
+        const Part& p = part[turn];
+        const int u0 = p.u0, u1 = p.u1, rows = p.rows, tile = p.tile, head = p.head;
+        const int64_t next = p.next;
+        const Seq& q = p.q;
+        // (the next part's description is there behind the part's last barriers)
+        auto look_ahead = [&]() {
+            while (next >= upto) { base = upto; upto = load_chunk<ROWS>(a, b0 += THREADS, base, chunk); }
+            __syncthreads();
+            if (warp == 0) find_part<ROWS>(a, chunk, next, end, part[turn ^ 1]);
+            __syncthreads();
+            entry = ask(part[turn ^ 1], 0);
+        };
+        if (u1 <= u0) {                                          // nothing but the item's head
+            if (next >= end) break;
+            look_ahead();
+            continue;
         }
-        const int64_t front = chunk.before[chunk.found], local = u - front, item = quotient(local, q.units);
-        const int g0 = (int)(local - item * q.units), g1 = (int)(q.units - g0 < end - u ? q.units : g0 + (end - u));
-        const int64_t here = u;
-        u += g1 - g0;
-        const int u0 = g0 > HEAD ? g0 - HEAD : 0, u1 = g1 - HEAD;
-        if (u1 <= u0) continue;                                  // nothing but the item's head
-        const int head = (int)quotient(item, q.tiles), tile = (int)(item - (int64_t)head * q.tiles);
-        const int rows = q.n * a.group - tile * ROWS < ROWS ? q.n * a.group - tile * ROWS : ROWS;   // of the tile
+        if (warp == 0 && next < end && next < upto) find_part<ROWS>(a, chunk, next, end, part[turn ^ 1]);
 
         // ---- the warp's slices, SL adjacent ones at a time: first + SL * WARPS * k + h
-        const int first = q.s0 + UNIT * u0 + SL * warp;
-        const int stop = q.s1 < q.s0 + UNIT * u1 ? q.s1 : q.s0 + UNIT * u1;
+        const int first = q.s0 + UNIT * u0 + SL * warp, stop = stop_of(p);
         const int count = first < stop ? (stop - first + SL * WARPS - 1) / (SL * WARPS) : 0;
-        int64_t place = -1;                                      // lane i: where the warp's slice number 32 * k + i lies
-        auto look_up = [&](int k) {
-            const int s = first + SL * WARPS * ((32 * k + lane) / SL) + (SL == 2 ? lane & 1 : 0);
-            place = -1;
-            if (s < stop) {
-                const int p = s / a.slices;
-                const int page = qp_kv_page(a.pages, q.slot, p * a.pages.page_size);
-                if (page >= 0) place = (((int64_t)page * a.heads + head) * a.slices + (s - p * a.slices)) * SB;
-                else flag = true;
-            }
-        };
+        int64_t place = place_of(p, 0, entry);
         int put = 0, take = 0;                                   // places in the ring
         auto issue = [&](int i) {                                // the warp's slice number i
             if (i < count * SL) {
-                if ((i & 31) == 0 && i > 0) look_up(i >> 5);
+                if ((i & 31) == 0 && i > 0) place = place_of(p, i >> 5, ask(p, i >> 5));
                 const int64_t from = __shfl_sync(0xFFFFFFFFu, place, i & 31);
                 if (lane == 0) sh_ok[warp][put] = from >= 0;
                 if (from >= 0) {
@@ -418,8 +482,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             }
             copies_close();
         };
-        // (the page numbers and the queries are asked for together, and the copies go out before the queries are looked at)
-        if (count > 0) look_up(0);
+        // (the queries are asked for, the copies go out, then the queries are looked at)
         float e[NT][D / 4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -438,7 +501,6 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         // ---- queries: operand registers and, per column, the factors of a score
         unsigned qb[NT][QB], ql[SPLIT ? NT : 1][SPLIT ? QB : 1];
         qp_f2 kf[NT], qs[NT];
-        int hi[NT][2];                                           // last key that the column's query sees
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             float top = 0.f, sum = 0.f;
@@ -470,18 +532,12 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             const float my_kf = a.scale_log2 / norm * (SPLIT ? 1.f : 16777216.f), my_qs = bad ? __int_as_float(0x7FC00000) : sum * a.scale_log2;
             kf[t] = qp_pack2(__shfl_sync(0xFFFFFFFFu, my_kf, 8 * j), __shfl_sync(0xFFFFFFFFu, my_kf, 8 * j + 4));
             qs[t] = qp_pack2(__shfl_sync(0xFFFFFFFFu, my_qs, 8 * j), __shfl_sync(0xFFFFFFFFu, my_qs, 8 * j + 4));
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                int rc = 8 * t + 2 * j + c;
-                rc = rc < rows ? rc : rows - 1;
-                hi[t][c] = q.pos + (tile * ROWS + rc) / a.group;
-            }
         }
+        if (lane < ROWS) sh_hi[warp][lane] = q.pos + (tile * ROWS + (lane < rows ? lane : rows - 1)) / a.group;
         // a slice inside [all_lo, all_hi) is seen whole by every query of the tile
         const int all_hi = q.pos + (tile * ROWS) / a.group + 1;
         const int last_i = (tile * ROWS + rows - 1) / a.group;
         const int all_lo = a.window > 0 ? q.pos + last_i - a.window + 1 : 0;
-        const int held = q.pos + q.n;                            // tokens behind are not written yet
 
         float o[NT][4 * VW][4];
         qp_f2 mn[NT], l[NT], lv[NT];                             // the reference, negated; sums of p and of p * lo'
@@ -550,7 +606,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                     kq[h] = *reinterpret_cast<const float2*>(x + S::KQ + (8 * h + tok) * 8);
                     vq[i][h] = *reinterpret_cast<const float2*>(x + S::VQ + (8 * h + tok) * 8);
                     // rows that were never written, or not copied, may hold anything
-                    if (!all && (!ok[i] || t0 + 16 * i + 8 * h + tok >= held)) kq[h] = vq[i][h] = make_float2(0.f, 0.f);
+                    if (!all && (!ok[i] || t0 + 16 * i + 8 * h + tok >= p.q.pos + p.q.n)) kq[h] = vq[i][h] = make_float2(0.f, 0.f);
                     if constexpr (SPLIT) {                       // the codes are less 8: lo is the value of code 8
                         kq[h].x = fmaf(8.f, kq[h].y, kq[h].x);
                         vq[i][h].x = fmaf(8.f, vq[i][h].y, vq[i][h].x);
@@ -573,7 +629,10 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                             const int key = t0 + 16 * i + 8 * h + tok;
 #pragma unroll
                             for (int c = 0; c < 2; ++c)
-                                if (!ok[i] || key > hi[t][c] || (a.window > 0 && key <= hi[t][c] - a.window)) y[c] = -__int_as_float(0x7F800000);
+                            {
+                                const int hi = sh_hi[warp][8 * t + 2 * j + c];
+                                if (!ok[i] || key > hi || (a.window > 0 && key <= hi - a.window)) y[c] = -__int_as_float(0x7F800000);
+                            }
                             s[i][t][h] = qp_pack2(y[0], y[1]);
                         }
             }
@@ -664,8 +723,14 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {                // codes 0..3, 4..7 of the word; both tokens of a pair in one register
                         const unsigned y = __byte_perm(w0[w], w1[w], h ? 0x7632 : 0x5410), z = __byte_perm(w2[w], w3[w], h ? 0x7632 : 0x5410);
-                        const unsigned c0 = codes<SPLIT>(y, M0), c1 = codes<SPLIT>(y >> 8, M0), c2 = codes<SPLIT>(z, M0), c3 = codes<SPLIT>(z >> 8, M0);
-                        const unsigned e0 = codes<SPLIT>(y, M1), e1 = codes<SPLIT>(y >> 8, M1), e2 = codes<SPLIT>(z, M1), e3 = codes<SPLIT>(z >> 8, M1);
+                        unsigned c0, c1, c2, c3, e0, e1, e2, e3;
+                        if constexpr (SPLIT) {
+                            c0 = codes<true>(y, M0); c1 = codes<true>(y >> 8, M0); c2 = codes<true>(z, M0); c3 = codes<true>(z >> 8, M0);
+                            e0 = codes<true>(y, M1); e1 = codes<true>(y >> 8, M1); e2 = codes<true>(z, M1); e3 = codes<true>(z >> 8, M1);
+                        } else {                                 // the odd code's sum comes with the even one's in a whole byte: one operation less
+                            e0 = y & 0x00FF00FFu; e1 = __byte_perm(y, 0u, 0x4341); e2 = z & 0x00FF00FFu; e3 = __byte_perm(z, 0u, 0x4341);
+                            c0 = y & M0; c1 = e1 & M0; c2 = z & M0; c3 = e3 & M0;
+                        }
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
                             if constexpr (SPLIT) {
@@ -689,6 +754,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         }
         copies_wait<0>();
         __syncthreads();                                         // the ring is free: it takes the warps' results
+        if (next < end && next < upto) entry = ask(part[turn ^ 1], 0);
 
         // ---- the block's result: O [warp][row][D], then m and l [warp][row]
         float* mo = reinterpret_cast<float*>(smem);
@@ -713,24 +779,24 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                 float* row = mo + (warp * ROWS + r) * D + n * (D / 8);
 #pragma unroll
                 for (int i = 0; i < 4 * VW; i += 2) {            // tiles i and i + 1: elements e, e + 2 and e + 1, e + 3 of word i / 4
-                    constexpr float f = SPLIT ? 1.f : 16777216.f;
+                    constexpr float f = SPLIT ? 1.f : 16777216.f, less = SPLIT ? 0.f : 1.f;
                     *reinterpret_cast<float4*>(row + 8 * (i >> 2) + 4 * ((i >> 1) & 1)) =
-                        make_float4(fmaf(o[t][i][c] * un, f, sv[c]), fmaf(o[t][i + 1][c] * un, f * 0.0625f, sv[c]),
-                                    fmaf(o[t][i][c + 2] * un, f, sv[c]), fmaf(o[t][i + 1][c + 2] * un, f * 0.0625f, sv[c]));
+                        make_float4(fmaf(o[t][i][c] * un, f, sv[c]), fmaf((o[t][i + 1][c] - less * o[t][i][c]) * un, f * 0.0625f, sv[c]),
+                                    fmaf(o[t][i][c + 2] * un, f, sv[c]), fmaf((o[t][i + 1][c + 2] - less * o[t][i][c + 2]) * un, f * 0.0625f, sv[c]));
                 }
             }
         }
         __syncthreads();
         const bool split = u0 > 0 || u1 < q.units - HEAD;
-        const int64_t i0 = here - g0;                            // the item's first unit; its blocks:
+        const int64_t i0 = p.u - p.g0;                           // the item's first unit; its blocks:
         int c0 = 0, c1 = 0, at = 0;
         if (split) {
             c0 = (int)quotient((i0 + HEAD + 1) * blocks - 1, W);
             c1 = (int)quotient((i0 + q.units) * blocks - 1, W);
             // a block's part of an item is its first if the item began in front of it or with it
-            at = 2 * (int)blockIdx.x + (here == begin ? 0 : 1);
+            at = 2 * (int)blockIdx.x + (p.u == begin ? 0 : 1);
         }
-        float* part = a.part + (int64_t)at * C::PART;
+        float* mine_at = a.part + (int64_t)at * C::PART;
         for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
             const int r = i / (D / 4), d = 4 * (i % (D / 4));
             float top = mm[r];
@@ -748,8 +814,8 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             if (!split) {
                 put_row<T, D>(a, q, head, tile * ROWS + r, d, so, top, sl);
             } else {
-                __stcg(reinterpret_cast<float4*>(part + r * D + d), so);
-                if (d == 0) { __stcg(part + ROWS * D + r, top); __stcg(part + ROWS * D + ROWS + r, sl); }
+                __stcg(reinterpret_cast<float4*>(mine_at + r * D + d), so);
+                if (d == 0) { __stcg(mine_at + ROWS * D + r, top); __stcg(mine_at + ROWS * D + ROWS + r, sl); }
             }
         }
         if (split) {
@@ -773,7 +839,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                 if (mine) add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, step, groups, nullptr, smem);
             }
         }
-        __syncthreads();                                         // shared memory is free for the next part
+        if (next >= end) break;
+        if (next >= upto) look_ahead();
+        else __syncthreads();                                    // shared memory is free for the next part
     }
     if (flag) atomicOr(a.status, QP_DEV_KV_RANGE);
 }
