@@ -4,9 +4,12 @@
 // min and max do not depend on the order they are taken in and every other step is one rounding, so the codes are
 // those of the token-wise calls bit for bit.  (A clip from sums, ACIQ, would depend on the order of the sum.)
 //
-// Eight lanes take the K and the V row of one (token, head): all loads go out before either row's reduction, min and
-// max need three shuffles, and the two quotients are one fp64 division with another numerator in every second lane.
-// Bound by the bytes: D elements in, D / 2 + 8 bytes out.
+// Eight lanes take the K and the V row of one (token, head): the loads of both go out before anything else, min and max need
+// three shuffles, and the four quotients of the two rows are one fp64 division, another one in every lane.  Rows without a NaN
+// or an infinity (found by one fused operation to two elements) need no clamp.  Bound by the bytes, D elements in, D / 2 + 8
+// bytes out, and by the instructions, about 12 to an element.  What keeps such a kernel from them is the chain of dependent loads batch -> position -> page -> row
+// (with the divisions between them 3 us, in every warp: 21 us for 8246 tokens of 8 heads), so one warp looks up a block's
+// tokens, a lane to a token, while the others' first rows are on their way.
 #include "qp_kv.cuh"
 
 QP_CK_UNIT
@@ -72,65 +75,105 @@ struct RowArgs {
     unsigned* status;
 };
 
-// where the slice and the row of a token and head are: 0 if nowhere (flag: the cache should have it)
-template <int D>
-__device__ __forceinline__ char* row_place(const RowArgs& a, int token, int head, int& row, bool& flag)
-{
-    const int b = qp_kv_find(a.rows, token);
-    if (b < 0) return nullptr;
-    const int first = __ldg(a.rows.pos + b);
-    if (first < 0) return nullptr;
-    const int64_t p = (int64_t)first + (token - qp_kv_start(a.rows, b));
-    const int page = p < (1ll << 31) - 1 ? qp_kv_page(a.pages, qp_kv_slot(a.rows, b), (int)p) : -1;
-    if (page < 0) { flag = true; return nullptr; }
-    const int in = (int)p % a.pages.page_size;
-    row = in % QP_KV_SLICE;
-    return a.pool + (((size_t)page * a.heads + head) * a.slices + in / QP_KV_SLICE) * qp_kv_slice<D>::BYTES;
-}
+constexpr int TOKENS = 32;                       // of a block, at most
+struct Places { int64_t at[TOKENS]; int row[TOKENS]; };
 
-template <int E>
-__device__ __forceinline__ void load_run(const float* p, bool vec, float (&e)[E])
+// Lane i < n: where token first + i's slice of head 0 begins and the row in it; -1 if nowhere (flag: the cache should have it).  The
+// first token's sequence by a 32-way search, the others' by steps from there.
+template <int D>
+__device__ __forceinline__ void look_up(const RowArgs& a, int first, int n, Places& to, bool& flag)
 {
-    if (vec) {
-#pragma unroll
-        for (int i = 0; i < E / 4; ++i) {
-            const float4 x = __ldcs(reinterpret_cast<const float4*>(p) + i);
-            e[4 * i] = x.x; e[4 * i + 1] = x.y; e[4 * i + 2] = x.z; e[4 * i + 3] = x.w;
+    const int lane = threadIdx.x & 31, token = first + lane;
+    const qp_kv_rows& r = a.rows;
+    int lo = first, hi = r.batch;
+    if (r.start) {
+        lo = 0;                                                  // the last b with start[b] <= first, or 0
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) >> 5, at = lo + lane * step;
+            const unsigned below = __ballot_sync(0xFFFFFFFFu, at < hi && (at == lo || qp_kv_start(r, at) <= first));
+            const int last = 31 - __clz(below);
+            hi = min(hi, lo + (last + 1) * step);
+            lo += last * step;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) e[i] = __ldcs(p + i);
     }
-}
-template <int E>
-__device__ __forceinline__ void load_run(const unsigned short* p, bool vec, float (&e)[E])
-{
-    if (vec) {
-#pragma unroll
-        for (int i = 0; i < E / 8; ++i) {
-            const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p) + i);
-            const unsigned w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                e[8 * i + 2 * h] = __uint_as_float(w[h] << 16);
-                e[8 * i + 2 * h + 1] = __uint_as_float(w[h] & 0xFFFF0000u);
+    int64_t place = -1;
+    int row = 0;
+    if (lane < n) {
+        int b = r.start ? lo : token, from = token;
+        if (r.start) {
+            from = qp_kv_start(r, b);
+            for (int next; b < r.batch && (next = qp_kv_start(r, b + 1)) <= token; from = next) ++b;
+        }
+        const int pos = b < r.batch && from <= token ? __ldg(r.pos + b) : -1;
+        if (pos >= 0) {
+            const int64_t p = (int64_t)pos + (token - from);
+            const int page = p < (1ll << 31) - 1 ? qp_kv_page(a.pages, qp_kv_slot(r, b), (int)p) : -1;
+            if (page < 0) {
+                flag = true;
+            } else {
+                const int in = (int)p % a.pages.page_size;
+                row = in % QP_KV_SLICE;
+                place = ((int64_t)page * a.heads * a.slices + in / QP_KV_SLICE) * qp_kv_slice<D>::BYTES;
             }
         }
-    } else {
+    }
+    to.at[lane] = place;
+    to.row[lane] = row;
+}
+
+// A lane's elements of a row: pieces sub, sub + 8, ... of 16 bytes, so that the eight lanes of a row meet whole sectors.
+template <typename T> constexpr int PIECE = 16 / sizeof(T);
+template <typename T, int E>
+__device__ __forceinline__ void load_run(const T* row, int sub, bool vec, float (&e)[E])
+{
+    constexpr int N = PIECE<T>;
 #pragma unroll
-        for (int i = 0; i < E; ++i) e[i] = qp_bf16_to_f32(__ldcs(p + i));
+    for (int i = 0; i < E / N; ++i) {
+        const T* p = row + (sub + 8 * i) * N;
+        if constexpr (sizeof(T) == 4) {
+            if (vec) {
+                const float4 x = __ldcs(reinterpret_cast<const float4*>(p));
+                e[4 * i] = x.x; e[4 * i + 1] = x.y; e[4 * i + 2] = x.z; e[4 * i + 3] = x.w;
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k) e[N * i + k] = __ldcs(p + k);
+            }
+        } else {
+            if (vec) {
+                const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p));
+                const unsigned w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                for (int h = 0; h < 4; ++h) {
+                    e[8 * i + 2 * h] = __uint_as_float(w[h] << 16);
+                    e[8 * i + 2 * h + 1] = __uint_as_float(w[h] & 0xFFFF0000u);
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < N; ++k) e[N * i + k] = qp_bf16_to_f32(__ldcs(p + k));
+            }
+        }
     }
 }
 
-// this lane's E elements of a row -> the row's quantizer and the lane's codes, 8 to a word
+// Ends of a row from the E elements that each of eight lanes has; whether all are finite.
 template <int E>
-__device__ __forceinline__ void quantize_run(float (&e)[E], int sub, unsigned (&words)[E / 8], float& lo, float& scale)
+__device__ __forceinline__ bool ends_of(const float (&e)[E], float& mn, float& mx)
 {
     const float inf = __int_as_float(0x7F800000);
-    float mn = inf, mx = -inf;
+    qp_f2 zero = qp_pack2(0.f, 0.f);                             // stays zero unless there is a NaN or an infinity
 #pragma unroll
-    for (int i = 0; i < E; ++i) { mn = fminf(mn, e[i]); mx = fmaxf(mx, e[i]); }       // (NaN is passed over)
-    if (mn == -inf || mx == inf) {                                                    // an infinity: over the finite ones
+    for (int i = 0; i < E; i += 2) zero = qp_fma2(qp_pack2(e[i], e[i + 1]), qp_pack2(0.f, 0.f), zero);
+    float z0, z1;
+    qp_unpack2(zero, z0, z1);
+    const bool fine = z0 == 0.f && z1 == 0.f;
+    mn = e[0];
+    mx = e[0];
+    if (fine) {
+#pragma unroll
+        for (int i = 1; i + 1 < E; i += 2) { mn = qp_min3(mn, e[i], e[i + 1]); mx = qp_max3(mx, e[i], e[i + 1]); }
+        mn = fminf(mn, e[E - 1]);
+        mx = fmaxf(mx, e[E - 1]);
+    } else {
         mn = inf; mx = -inf;
 #pragma unroll
         for (int i = 0; i < E; ++i)
@@ -142,161 +185,203 @@ __device__ __forceinline__ void quantize_run(float (&e)[E], int sub, unsigned (&
         mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, o, 8));
     }
     if (mn > mx) mn = mx = 0.f;                                                       // nothing finite
-    const double width = (double)mx - (double)mn;
+    return fine;
+}
+
+// Quantizers of the two rows with the ends given: scale and inv_scale
+__device__ __forceinline__ void quotients(float k_mn, float k_mx, float v_mn, float v_mx, int sub, float (&scale)[2], float (&inv)[2])
+{
+    const double width = sub & 2 ? (double)v_mx - (double)v_mn : (double)k_mx - (double)k_mn;
     const bool odd = sub & 1;
-    const float mine = (float)((odd ? 15.0 : width) / (odd ? width : 15.0));          // even lanes: scale, odd lanes: inv_scale
-    const float other = __shfl_xor_sync(0xFFFFFFFFu, mine, 1, 8);
-    float inv = odd ? mine : other;
-    lo = mn;
-    scale = odd ? other : mine;
-    if (!(inv < inf)) { scale = 0.f; inv = 0.f; }                                     // constant, or too narrow for inv_scale
+    const float mine = (float)((odd ? 15.0 : width) / (odd ? width : 15.0));          // lanes 0, 2: scales, lanes 1, 3: inv_scales
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        scale[h] = __shfl_sync(0xFFFFFFFFu, mine, 2 * h, 8);
+        inv[h] = __shfl_sync(0xFFFFFFFFu, mine, 2 * h + 1, 8);
+        if (!(inv[h] < __int_as_float(0x7F800000))) { scale[h] = 0.f; inv[h] = 0.f; }  // constant, or too narrow for inv_scale
+    }
+}
+
+// the lane's codes, a quad of four to 16 bits
+template <int E>
+__device__ __forceinline__ void codes_of(float (&e)[E], bool fine, float mn, float mx, float inv, unsigned (&quads)[E / 4])
+{
     float l = mn, h = mx;
-    if (__fsub_rn(mx, mn) == inf) {                                                   // the range passes fp32: halves
+    const bool wide = __fsub_rn(mx, mn) == __int_as_float(0x7F800000);                // the range passes fp32: halves
+    if (wide) {
         l *= 0.5f; h *= 0.5f; inv *= 2.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) e[i] *= 0.5f;
     }
+    if (__all_sync(0xFFFFFFFFu, fine)) {
+        // qp_quad without its clamp: every element lies between the ends
+        const qp_f2 nl = qp_pack2(-l, -l), inv2 = qp_pack2(inv, inv), magic = qp_pack2(QP_MAGIC, QP_MAGIC);
+        constexpr unsigned offs = QP_MAGIC_BITS * 0x1111u;
 #pragma unroll
-    for (int i = 0; i < E / 8; ++i) words[i] = qp_quad<4>(e + 8 * i, l, h, inv) | (qp_quad<4>(e + 8 * i + 4, l, h, inv) << 16);
+        for (int i = 0; i < E / 4; ++i) {
+            float a, b, c, d;
+            qp_unpack2(qp_add2(qp_mul2(qp_add2(qp_pack2(e[4 * i], e[4 * i + 1]), nl), inv2), magic), a, b);
+            qp_unpack2(qp_add2(qp_mul2(qp_add2(qp_pack2(e[4 * i + 2], e[4 * i + 3]), nl), inv2), magic), c, d);
+            // (the sum of four shifted words, less the sum of the shifted constants)
+            quads[i] = (__float_as_uint(a) + (__float_as_uint(b) << 4)) + ((__float_as_uint(c) << 8) + (__float_as_uint(d) << 12)) - offs;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < E / 4; ++i) quads[i] = qp_quad<4>(e + 4 * i, l, h, inv);
+    }
 }
 
-template <int W>
-__device__ __forceinline__ void put_words(char* p, const unsigned (&w)[W])
+// a lane's codes of a row, to and from the cache: pieces as load_run has them
+template <typename T, int Q>
+__device__ __forceinline__ void put_codes(char* row, int sub, const unsigned (&q)[Q])
 {
-    if constexpr (W == 1) *reinterpret_cast<unsigned*>(p) = w[0];
-    else if constexpr (W == 2) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+    for (int i = 0; i < Q; i += PIECE<T> / 4) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<unsigned short*>(row + (sub + 8 * i) * 2) = (unsigned short)q[i];
+        else *reinterpret_cast<unsigned*>(row + (sub + 4 * i) * 4) = q[i] | (q[i + 1] << 16);
+    }
 }
-template <int W>
-__device__ __forceinline__ void get_words(const char* p, unsigned (&w)[W])
+template <typename T, int Q>
+__device__ __forceinline__ void get_codes(const char* row, int sub, unsigned (&q)[Q])
 {
-    if constexpr (W == 1) w[0] = *reinterpret_cast<const unsigned*>(p);
-    else if constexpr (W == 2) { const uint2 x = *reinterpret_cast<const uint2*>(p); w[0] = x.x; w[1] = x.y; }
-    else { const uint4 x = *reinterpret_cast<const uint4*>(p); w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w; }
+#pragma unroll
+    for (int i = 0; i < Q; i += PIECE<T> / 4) {
+        if constexpr (sizeof(T) == 4) {
+            q[i] = *reinterpret_cast<const unsigned short*>(row + (sub + 8 * i) * 2);
+        } else {
+            const unsigned w = *reinterpret_cast<const unsigned*>(row + (sub + 4 * i) * 4);
+            q[i] = w & 0xFFFFu;
+            q[i + 1] = w >> 16;
+        }
+    }
 }
 
-constexpr int ROWS = QP_THREADS / 8;
+constexpr int GROUPS = QP_THREADS / 8;
 
-// whole groups of eight lanes take part in every round, so the shuffles are never divergent
+// a block's tokens: first = blockIdx.x * per_block, at most per_block of them
 template <typename T, int D>
-__global__ void __launch_bounds__(QP_THREADS) kv_append_kernel(const RowArgs a, int n, bool vec)
+__global__ void __launch_bounds__(QP_THREADS) kv_append_kernel(const RowArgs a, int per_block, bool vec)
 {
     constexpr int E = D / 8;
     using S = qp_kv_slice<D>;
-    const int sub = threadIdx.x & 7;
+    __shared__ Places places;
+    const int sub = threadIdx.x & 7, group = threadIdx.x >> 3;
+    const int first = blockIdx.x * per_block, n = min(per_block, a.rows.tokens - first), pairs = n * a.heads;
     bool flag = false;
-    for (int r0 = blockIdx.x * ROWS; r0 < n; r0 += gridDim.x * ROWS) {
-        const int r = r0 + (threadIdx.x >> 3);
-        const int token = r / a.heads, head = r - token * a.heads;
-        int row = 0;
-        char* s = r < n ? row_place<D>(a, token, head, row, flag) : nullptr;
+    for (int i0 = 0; i0 < pairs; i0 += GROUPS) {                 // whole groups of eight lanes take part in every round
+        const int i = i0 + group, in = i / a.heads, head = i - in * a.heads;
+        const int64_t token = first + in;
         float k[E], v[E];
-        if (s) {
-            load_run(static_cast<const T*>(a.k) + token * a.kt + head * a.kh + sub * E, vec, k);
-            load_run(static_cast<const T*>(a.v) + token * a.vt + head * a.vh + sub * E, vec, v);
+        if (i < pairs) {
+            load_run(static_cast<const T*>(a.k) + token * a.kt + head * a.kh, sub, vec, k);
+            load_run(static_cast<const T*>(a.v) + token * a.vt + head * a.vh, sub, vec, v);
         } else {
 #pragma unroll
-            for (int i = 0; i < E; ++i) k[i] = v[i] = 0.f;
+            for (int e = 0; e < E; ++e) k[e] = v[e] = 0.f;
         }
-        unsigned w[E / 8];
-        float lo, scale;
-        quantize_run(k, sub, w, lo, scale);
-        if (s) {
-            put_words(s + row * S::ROW + sub * (E / 2), w);
-            if (sub == 0) *reinterpret_cast<float2*>(s + S::KQ + row * 8) = make_float2(lo, scale);
+        if (i0 == 0) {
+            if (threadIdx.x < 32) look_up<D>(a, first, n, places, flag);
+            __syncthreads();
         }
-        quantize_run(v, sub, w, lo, scale);
-        if (s) {
-            put_words(s + S::V + row * S::ROW + sub * (E / 2), w);
-            if (sub == 0) *reinterpret_cast<float2*>(s + S::VQ + row * 8) = make_float2(lo, scale);
+        const int64_t place = i < pairs ? places.at[in] : -1;
+        const int row = i < pairs ? places.row[in] : 0;
+        char* s = a.pool + place + (int64_t)head * a.slices * S::BYTES;
+        float k_mn, k_mx, v_mn, v_mx, scale[2], inv[2];
+        const bool k_fine = ends_of(k, k_mn, k_mx), v_fine = ends_of(v, v_mn, v_mx);
+        quotients(k_mn, k_mx, v_mn, v_mx, sub, scale, inv);
+        unsigned kw[E / 4], vw[E / 4];
+        codes_of(k, k_fine, k_mn, k_mx, inv[0], kw);
+        codes_of(v, v_fine, v_mn, v_mx, inv[1], vw);
+        if (place >= 0) {
+            put_codes<T>(s + row * S::ROW, sub, kw);
+            put_codes<T>(s + S::V + row * S::ROW, sub, vw);
+            if (sub < 2) *reinterpret_cast<float2*>(s + (sub ? S::VQ : S::KQ) + row * 8) = make_float2(sub ? v_mn : k_mn, sub ? scale[1] : scale[0]);
         }
     }
     if (flag) atomicOr(a.status, QP_DEV_KV_RANGE);
 }
 
-template <int E>
-__device__ __forceinline__ void store_run(float* p, bool vec, const float (&e)[E])
+template <typename T, int E>
+__device__ __forceinline__ void store_run(T* row, int sub, bool vec, const float (&e)[E])
 {
-    if (vec) {
+    constexpr int N = PIECE<T>;
 #pragma unroll
-        for (int i = 0; i < E / 4; ++i) __stcs(reinterpret_cast<float4*>(p) + i, make_float4(e[4 * i], e[4 * i + 1], e[4 * i + 2], e[4 * i + 3]));
-    } else {
+    for (int i = 0; i < E / N; ++i) {
+        T* p = row + (sub + 8 * i) * N;
+        if constexpr (sizeof(T) == 4) {
+            if (vec) {
+                __stcs(reinterpret_cast<float4*>(p), make_float4(e[4 * i], e[4 * i + 1], e[4 * i + 2], e[4 * i + 3]));
+            } else {
 #pragma unroll
-        for (int i = 0; i < E; ++i) p[i] = e[i];
-    }
-}
-template <int E>
-__device__ __forceinline__ void store_run(unsigned short* p, bool vec, const float (&e)[E])
-{
-    unsigned short h[E];
+                for (int k = 0; k < N; ++k) p[k] = e[N * i + k];
+            }
+        } else {
+            unsigned h[4];
 #pragma unroll
-    for (int i = 0; i < E; ++i) h[i] = qp_f32_to_bf16(e[i]);
-    if (vec) {
+            for (int k = 0; k < 4; ++k) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(h[k]) : "f"(e[8 * i + 2 * k + 1]), "f"(e[8 * i + 2 * k]));
+            if (vec) {
+                __stcs(reinterpret_cast<uint4*>(p), make_uint4(h[0], h[1], h[2], h[3]));
+            } else {
 #pragma unroll
-        for (int i = 0; i < E / 8; ++i) {
-            uint4 x;
-            x.x = h[8 * i] | ((unsigned)h[8 * i + 1] << 16);
-            x.y = h[8 * i + 2] | ((unsigned)h[8 * i + 3] << 16);
-            x.z = h[8 * i + 4] | ((unsigned)h[8 * i + 5] << 16);
-            x.w = h[8 * i + 6] | ((unsigned)h[8 * i + 7] << 16);
-            __stcs(reinterpret_cast<uint4*>(p) + i, x);
+                for (int k = 0; k < N; ++k) p[k] = (unsigned short)(h[k / 2] >> (16 * (k & 1)));
+            }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < E; ++i) p[i] = h[i];
     }
 }
 
+// A code under 128's exponent (at bits 16..19) or 2048's (at bits 12..15) is that number + code; less the number, exactly the code.
 template <int E>
-__device__ __forceinline__ void values_of(const unsigned (&w)[E / 8], float2 q, float (&e)[E])
+__device__ __forceinline__ void values_of(const unsigned (&q)[E / 4], float2 quant, float (&e)[E])
 {
+    const qp_f2 less = qp_pack2(-2048.f, -128.f), scale = qp_pack2(quant.y, quant.y), lo = qp_pack2(quant.x, quant.x);
 #pragma unroll
-    for (int i = 0; i < E; ++i) e[i] = fmaf((float)((w[i / 8] >> (4 * (i & 7))) & 15u), q.y, q.x);
+    for (int i = 0; i < E / 4; ++i) {
+        const unsigned a = q[i] << 12, b = q[i] << 4;            // codes 0, 1 and 2, 3 at bits 12..19
+        qp_unpack2(qp_fma2(qp_add2(qp_pack2(__uint_as_float((a & 0xF000u) | 0x45000000u), __uint_as_float((a & 0xF0000u) | 0x43000000u)), less), scale, lo),
+                   e[4 * i], e[4 * i + 1]);
+        qp_unpack2(qp_fma2(qp_add2(qp_pack2(__uint_as_float((b & 0xF000u) | 0x45000000u), __uint_as_float((b & 0xF0000u) | 0x43000000u)), less), scale, lo),
+                   e[4 * i + 2], e[4 * i + 3]);
+    }
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(QP_THREADS) kv_gather_kernel(const RowArgs a, int n, bool vec)
+__global__ void __launch_bounds__(QP_THREADS) kv_gather_kernel(const RowArgs a, int per_block, bool vec)
 {
     constexpr int E = D / 8;
     using S = qp_kv_slice<D>;
-    const int sub = threadIdx.x & 7;
+    __shared__ Places places;
+    const int sub = threadIdx.x & 7, group = threadIdx.x >> 3;
+    const int first = blockIdx.x * per_block, n = min(per_block, a.rows.tokens - first), pairs = n * a.heads;
     bool flag = false;
-    for (int r = blockIdx.x * ROWS + (threadIdx.x >> 3); r < n; r += gridDim.x * ROWS) {
-        const int token = r / a.heads, head = r - token * a.heads;
-        int row = 0;
-        const char* s = row_place<D>(a, token, head, row, flag);
-        if (!s) continue;
-        unsigned kw[E / 8], vw[E / 8];
-        get_words(s + row * S::ROW + sub * (E / 2), kw);
-        get_words(s + S::V + row * S::ROW + sub * (E / 2), vw);
+    if (threadIdx.x < 32) look_up<D>(a, first, n, places, flag);
+    __syncthreads();
+#pragma unroll 2
+    for (int i = group; i < pairs; i += GROUPS) {
+        const int in = i / a.heads, head = i - in * a.heads, row = places.row[in];
+        const int64_t token = first + in, place = places.at[in];
+        if (place < 0) continue;
+        const char* s = a.pool + place + (int64_t)head * a.slices * S::BYTES;
+        unsigned kw[E / 4], vw[E / 4];
+        get_codes<T>(s + row * S::ROW, sub, kw);
+        get_codes<T>(s + S::V + row * S::ROW, sub, vw);
         const float2 kq = *reinterpret_cast<const float2*>(s + S::KQ + row * 8), vq = *reinterpret_cast<const float2*>(s + S::VQ + row * 8);
         float e[E];
         if (a.k) {
             values_of(kw, kq, e);
-            store_run(const_cast<T*>(static_cast<const T*>(a.k)) + token * a.kt + head * a.kh + sub * E, vec, e);
+            store_run(const_cast<T*>(static_cast<const T*>(a.k)) + token * a.kt + head * a.kh, sub, vec, e);
         }
         if (a.v) {
             values_of(vw, vq, e);
-            store_run(const_cast<T*>(static_cast<const T*>(a.v)) + token * a.vt + head * a.vh + sub * E, vec, e);
+            store_run(const_cast<T*>(static_cast<const T*>(a.v)) + token * a.vt + head * a.vh, sub, vec, e);
         }
     }
     if (flag) atomicOr(a.status, QP_DEV_KV_RANGE);
 }
 
 typedef void (*RowKernel)(const RowArgs, int, bool);
-
-template <template <typename, int> class K>
-RowKernel pick(int dtype, int d);
-
-template <typename T, int D> struct AppendOf { static RowKernel get() { return kv_append_kernel<T, D>; } };
-template <typename T, int D> struct GatherOf { static RowKernel get() { return kv_gather_kernel<T, D>; } };
-
-template <template <typename, int> class K>
-RowKernel pick(int dtype, int d)
-{
-    if (dtype == QP_F32) return d == 64 ? K<float, 64>::get() : d == 128 ? K<float, 128>::get() : K<float, 256>::get();
-    return d == 64 ? K<unsigned short, 64>::get() : d == 128 ? K<unsigned short, 128>::get() : K<unsigned short, 256>::get();
-}
+template <typename T, int D> RowKernel kernel_of(bool append) { return append ? kv_append_kernel<T, D> : kv_gather_kernel<T, D>; }
+template <typename T>
+RowKernel pick(bool append, int d) { return d == 64 ? kernel_of<T, 64>(append) : d == 128 ? kernel_of<T, 128>(append) : kernel_of<T, 256>(append); }
 
 int32_t launch_rows(qp_ctx* ctx, bool append, const qp_kv_cache_t* c, const qp_kv_batch_t* b, int layer, const void* k, const void* v,
                     int dtype, int64_t kt, int64_t kh, int64_t vt, int64_t vh, void* stream)
@@ -325,10 +410,12 @@ int32_t launch_rows(qp_ctx* ctx, bool append, const qp_kv_cache_t* c, const qp_k
     a.k = k; a.v = v;
     a.kt = kt; a.kh = kh; a.vt = vt; a.vh = vh;
     a.status = ctx->d_status;
-    const int n = b->tokens * c->heads;
-    const uint64_t want = ((uint64_t)n + ROWS - 1) / ROWS, cap = (uint64_t)ctx->sm_count * 64;
-    const RowKernel f = append ? pick<AppendOf>(dtype, c->head_dim) : pick<GatherOf>(dtype, c->head_dim);
-    f<<<(unsigned)(want < cap ? want : cap), QP_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a, n, vec);
+    // Four rounds to a block at most (128 pairs of token and head), and enough blocks for two on every SM where there are the tokens
+    int per_block = 4 * GROUPS / c->heads, fill = (b->tokens + 2 * ctx->sm_count - 1) / (2 * ctx->sm_count);
+    if (per_block > fill) per_block = fill;
+    per_block = per_block < 1 ? 1 : per_block > TOKENS ? TOKENS : per_block;
+    const RowKernel f = dtype == QP_F32 ? pick<float>(append, c->head_dim) : pick<unsigned short>(append, c->head_dim);
+    f<<<(unsigned)((b->tokens + per_block - 1) / per_block), QP_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a, per_block, vec);
     ctx->launches += 1;
     return qp_check_launch(ctx, append ? "qp_kv_append" : "qp_kv_gather");
 }
