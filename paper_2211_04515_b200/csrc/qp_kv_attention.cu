@@ -161,7 +161,7 @@ template <int ROWS>
 __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
 {
     Seq q;
-    q.pos = __ldg(a.rows.pos + b);
+    q.pos = qp_kv_ld(a.rows.pos + b);
     q.slot = qp_kv_slot(a.rows, b);
     q.row0 = qp_kv_start(a.rows, b);
     const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
@@ -249,14 +249,14 @@ __device__ __forceinline__ void load_q(const unsigned short* p, bool vec, float 
     if (vec) {
 #pragma unroll
         for (int i = 0; i < N / 8; ++i) {
-            const uint4 x = __ldg(reinterpret_cast<const uint4*>(p) + i);
+            const uint4 x = qp_kv_ld(reinterpret_cast<const uint4*>(p) + i);
             const unsigned w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
             for (int h = 0; h < 4; ++h) { e[8 * i + 2 * h] = __uint_as_float(w[h] << 16); e[8 * i + 2 * h + 1] = __uint_as_float(w[h] & 0xFFFF0000u); }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) e[i] = qp_bf16_to_f32(__ldg(p + i));
+        for (int i = 0; i < N; ++i) e[i] = qp_bf16_to_f32(qp_kv_ld(p + i));
     }
 }
 template <int N>
@@ -265,12 +265,12 @@ __device__ __forceinline__ void load_q(const float* p, bool vec, float (&e)[N])
     if (vec) {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) {
-            const float4 x = __ldg(reinterpret_cast<const float4*>(p) + i);
+            const float4 x = qp_kv_ld(reinterpret_cast<const float4*>(p) + i);
             e[4 * i] = x.x; e[4 * i + 1] = x.y; e[4 * i + 2] = x.z; e[4 * i + 3] = x.w;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) e[i] = __ldg(p + i);
+        for (int i = 0; i < N; ++i) e[i] = qp_kv_ld(p + i);
     }
 }
 __device__ __forceinline__ void put_out(float* p, bool vec, const float (&v)[4])
@@ -394,6 +394,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     constexpr int QB = 4 * KW;                                   // operand registers of a query tile
     constexpr unsigned M0 = 0x000F000Fu, M1 = 0x00F000F0u;
     extern __shared__ __align__(16) char smem[];
+    qp_kv_begin();
     __shared__ Chunk chunk;
     __shared__ Part part[2];
     __shared__ int sh_ok[WARPS][STAGES], sh_hi[WARPS][ROWS];    // slices that are there; last key that a query sees
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     auto ask = [&](const Part& p, int k) {
         const int s = slice_of(p, k), i = s / a.slices;
         const bool in = s < stop_of(p) && (unsigned)p.q.slot < (unsigned)a.pages.max_seqs && i < a.pages.max_pages;
-        return in ? __ldg(a.pages.table + (size_t)p.q.slot * a.pages.max_pages + i) : -1;
+        return in ? qp_kv_ld(a.pages.table + (size_t)p.q.slot * a.pages.max_pages + i) : -1;
     };
     auto place_of = [&](const Part& p, int k, int page) {
         const int s = slice_of(p, k);
@@ -847,7 +848,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
 }
 
 struct Launch {
-    const void* kernel;
+    void (*kernel)(const qp_kv_attn_args);
     int smem, per_sm, rows;
     bool* ready;
 };
@@ -857,7 +858,7 @@ Launch launch_of()
 {
     static bool ready[QP_KV_MAX_DEVICES];
     using C = Cfg<D, NT, SPLIT>;
-    return {reinterpret_cast<const void*>(kv_attn_kernel<D, NT, SPLIT>), C::SMEM, C::PER_SM, C::ROWS, ready};
+    return {kv_attn_kernel<D, NT, SPLIT>, C::SMEM, C::PER_SM, C::ROWS, ready};
 }
 
 // rows: queries to a cached head, at most
@@ -941,8 +942,7 @@ extern "C" int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, co
             return qp_check_launch(ctx, "qp_kv_attention (shared memory)");
         if (ctx->device < QP_KV_MAX_DEVICES) f.ready[ctx->device] = true;
     }
-    void* args[] = {&a};
-    cudaLaunchKernel(f.kernel, dim3((unsigned)grid), dim3(THREADS), args, (size_t)f.smem, s);
+    qp_kv_launch(f.kernel, (unsigned)grid, THREADS, (size_t)f.smem, s, a);
     ctx->launches += 1;
     return qp_check_launch(ctx, "qp_kv_attention");
 }

@@ -204,7 +204,7 @@ struct Seq { int pos, n, row0, slot, tiles; };
 __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
 {
     Seq q;
-    q.pos = __ldg(a.rows.pos + b);
+    q.pos = qp_kv_ld(a.rows.pos + b);
     q.slot = qp_kv_slot(a.rows, b);
     q.row0 = qp_kv_start(a.rows, b);
     const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
@@ -335,15 +335,15 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
             for (int l = 0; l < L; ++l) {
                 const int64_t at = __shfl_sync(0xFFFFFFFFu, place, (l * 128 + p) / PER);
                 const char* from = a.pool + at + row * S::ROW + piece * 16;
-                x.k[l] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
-                x.v[l] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(from + S::V)) : make_uint4(0, 0, 0, 0);
+                x.k[l] = at >= 0 ? qp_kv_ld(reinterpret_cast<const uint4*>(from)) : make_uint4(0, 0, 0, 0);
+                x.v[l] = at >= 0 ? qp_kv_ld(reinterpret_cast<const uint4*>(from + S::V)) : make_uint4(0, 0, 0, 0);
             }
             const int64_t mine = __shfl_sync(0xFFFFFFFFu, place, p / QP_KV_SLICE);
             x.quant = make_float4(0.f, 0.f, 0.f, 0.f);
             const bool there = mine >= 0 && (s.s0 + 8 * u) * QP_KV_SLICE + p < held;
             if (there) {
-                const float2 kq = __ldg(reinterpret_cast<const float2*>(a.pool + mine + S::KQ + p % QP_KV_SLICE * 8));
-                const float2 vq = __ldg(reinterpret_cast<const float2*>(a.pool + mine + S::VQ + p % QP_KV_SLICE * 8));
+                const float2 kq = qp_kv_ld(reinterpret_cast<const float2*>(a.pool + mine + S::KQ + p % QP_KV_SLICE * 8));
+                const float2 vq = qp_kv_ld(reinterpret_cast<const float2*>(a.pool + mine + S::VQ + p % QP_KV_SLICE * 8));
                 x.quant = make_float4(kq.x, kq.y, vq.x, vq.y);
             }
             x.there = __ballot_sync(0xFFFFFFFFu, there);
@@ -519,13 +519,13 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
                 for (int c = 0; c < D / 8; ++c) x[c] = make_uint4(0, 0, 0, 0);
             } else if (a.vec) {
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) x[c] = __ldg(reinterpret_cast<const uint4*>(from) + c);
+                for (int c = 0; c < D / 8; ++c) x[c] = qp_kv_ld(reinterpret_cast<const uint4*>(from) + c);
             } else {
 #pragma unroll
                 for (int c = 0; c < D / 8; ++c) {
                     unsigned w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[e] = __ldg(from + 8 * c + 2 * e) | ((unsigned)__ldg(from + 8 * c + 2 * e + 1) << 16);
+                    for (int e = 0; e < 4; ++e) w[e] = qp_kv_ld(from + 8 * c + 2 * e) | ((unsigned)qp_kv_ld(from + 8 * c + 2 * e + 1) << 16);
                     x[c] = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
@@ -769,6 +769,7 @@ __global__ void __launch_bounds__(THREADS, 1) kv_chunk_kernel(const qp_kv_attn_a
 {
     using C = Cfg<D>;
     extern __shared__ char raw[];
+    qp_kv_begin();
     __shared__ Shared sh;
     char* smem = raw + ((1024u - (smem_of(raw) & 1023u)) & 1023u);
     char* stages = smem + 2 * C::OPERAND;
@@ -874,7 +875,7 @@ uint64_t qp_kv_chunk_part_bytes(int head_dim, int sm_count)
 int32_t qp_kv_chunk_launch(qp_ctx* ctx, const qp_kv_attn_args& a, int head_dim, cudaStream_t s)
 {
     static bool ready[2][QP_KV_MAX_DEVICES];
-    const void* f = head_dim == 64 ? reinterpret_cast<const void*>(kv_chunk_kernel<64>) : reinterpret_cast<const void*>(kv_chunk_kernel<128>);
+    void (*f)(const qp_kv_attn_args) = head_dim == 64 ? kv_chunk_kernel<64> : kv_chunk_kernel<128>;
     const int smem = head_dim == 64 ? Cfg<64>::SMEM : Cfg<128>::SMEM;
     bool* done = ctx->device < QP_KV_MAX_DEVICES ? &ready[head_dim == 128][ctx->device] : nullptr;
     if (!done || !*done) {
@@ -882,8 +883,7 @@ int32_t qp_kv_chunk_launch(qp_ctx* ctx, const qp_kv_attn_args& a, int head_dim, 
             return qp_check_launch(ctx, "qp_kv_attention (shared memory)");
         if (done) *done = true;
     }
-    void* args[] = {const_cast<qp_kv_attn_args*>(&a)};
-    cudaLaunchKernel(f, dim3((unsigned)ctx->sm_count), dim3(THREADS), args, (size_t)smem, s);
+    qp_kv_launch(f, (unsigned)ctx->sm_count, THREADS, (size_t)smem, s, a);
     ctx->launches += 1;
     return qp_check_launch(ctx, "qp_kv_attention");
 }

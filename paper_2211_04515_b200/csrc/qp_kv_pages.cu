@@ -106,12 +106,12 @@ __device__ __forceinline__ volatile int* claim_slots(const Cache& c, const int32
 {
     volatile int* claim = c.max_seqs <= SMEM_CLAIMS ? sh_claim : c.s0;
     for (int i = threadIdx.x; i < n; i += PLAN) {
-        const int s = __ldg(slots + i);
+        const int s = qp_kv_ld(slots + i);
         if (s >= 0 && s < c.max_seqs) claim[s] = NONE;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += PLAN) {
-        const int s = __ldg(slots + i);
+        const int s = qp_kv_ld(slots + i);
         if (s >= 0 && s < c.max_seqs) atomicMin(const_cast<int*>(claim) + s, i);
     }
     __syncthreads();
@@ -120,10 +120,11 @@ __device__ __forceinline__ volatile int* claim_slots(const Cache& c, const int32
 
 // ---------------------------------------------------------------------------- growing
 
-__global__ void __launch_bounds__(PLAN) kv_extend_kernel(const Cache c, const int32_t* __restrict__ slots,
-                                                         const int32_t* __restrict__ start, int32_t* __restrict__ pos, int batch,
+__global__ void __launch_bounds__(PLAN) kv_extend_kernel(const Cache c, const int32_t* slots,
+                                                         const int32_t* start, int32_t* pos, int batch,
                                                          int tokens, int max_new)
 {
+    qp_kv_begin();
     __shared__ int sh[PW + 1], sh_claim[SMEM_CLAIMS], sh_taken[SMEM_TAKEN];
     volatile int* claim = slots ? claim_slots(c, slots, batch, sh_claim) : nullptr;
     bool range = false;
@@ -132,10 +133,10 @@ __global__ void __launch_bounds__(PLAN) kv_extend_kernel(const Cache c, const in
         const int b = b0 + threadIdx.x;
         int need = 0, old = -1;
         if (b < batch) {
-            const int s = slots ? __ldg(slots + b) : b;
+            const int s = slots ? qp_kv_ld(slots + b) : b;
             int64_t n = 1;
             if (start) {
-                const int64_t s0 = __ldg(start + b), s1 = __ldg(start + b + 1);
+                const int64_t s0 = qp_kv_ld(start + b), s1 = qp_kv_ld(start + b + 1);
                 n = s1 - s0;
                 if (s0 < 0 || n < 0 || s1 > tokens) n = -1;
             } else if (b >= tokens) {
@@ -171,14 +172,14 @@ __global__ void __launch_bounds__(PLAN) kv_extend_kernel(const Cache c, const in
                 const int mid = (lo + hi) >> 1;
                 if (c.s1[mid] <= k) lo = mid; else hi = mid;
             }
-            const int s = slots ? __ldg(slots + lo) : lo;
+            const int s = slots ? qp_kv_ld(slots + lo) : lo;
             c.table[(size_t)s * c.max_pages + pages_of(c.s2[lo], c.page_size) + (k - c.s1[lo])] = taken[k];
             c.refs[taken[k]] = 1;
         }
         for (int b = threadIdx.x; b < batch; b += PLAN) {
             const int old = c.s2[b];
             pos[b] = old;
-            if (old >= 0) c.lens[slots ? __ldg(slots + b) : b] = old + (start ? __ldg(start + b + 1) - __ldg(start + b) : 1);
+            if (old >= 0) c.lens[slots ? qp_kv_ld(slots + b) : b] = old + (start ? qp_kv_ld(start + b + 1) - qp_kv_ld(start + b) : 1);
         }
     }
     if (range) atomicOr(c.status, QP_DEV_KV_RANGE);
@@ -186,11 +187,12 @@ __global__ void __launch_bounds__(PLAN) kv_extend_kernel(const Cache c, const in
 
 // ---------------------------------------------------------------------------- freeing
 
-__global__ void __launch_bounds__(128) kv_free_kernel(const Cache c, const int32_t* __restrict__ slots, int n)
+__global__ void __launch_bounds__(128) kv_free_kernel(const Cache c, const int32_t* slots, int n)
 {
+    qp_kv_begin();
     __shared__ int sh_len;
     for (int i = blockIdx.x; i < n; i += gridDim.x) {
-        const int s = __ldg(slots + i);
+        const int s = qp_kv_ld(slots + i);
         if (s < 0 || s >= c.max_seqs) {
             if (threadIdx.x == 0) atomicOr(c.status, QP_DEV_KV_RANGE);
             continue;
@@ -255,6 +257,7 @@ __device__ __forceinline__ void move_piece(const Moves& m, int64_t t)
 
 __global__ void __launch_bounds__(MOVE_THREADS) kv_move_kernel(const Moves m, int n)
 {
+    qp_kv_begin();
     const int64_t pieces = (int64_t)n * m.layers * m.chunks;
     for (int64_t t = blockIdx.x; t < pieces; t += gridDim.x) move_piece(m, t);
 }
@@ -281,9 +284,10 @@ unsigned move_grid(const qp_ctx* ctx, int64_t tasks)
 // ---------------------------------------------------------------------------- forking
 
 // Pair i: s2[i] = tokens it copies (-1: it is skipped), a[i], b[i] = the part-filled page and the page that takes its copy (-1: none)
-__global__ void __launch_bounds__(PLAN) kv_fork_plan_kernel(const Cache c, const int32_t* __restrict__ src,
-                                                            const int32_t* __restrict__ dst, int n)
+__global__ void __launch_bounds__(PLAN) kv_fork_plan_kernel(const Cache c, const int32_t* src,
+                                                            const int32_t* dst, int n)
 {
+    qp_kv_begin();
     __shared__ int sh[PW + 1], sh_claim[SMEM_CLAIMS];
     volatile int* claim = claim_slots(c, dst, n, sh_claim);
     bool range = false;
@@ -292,7 +296,7 @@ __global__ void __launch_bounds__(PLAN) kv_fork_plan_kernel(const Cache c, const
         const int i = i0 + threadIdx.x;
         int len = -1, tail = 0;
         if (i < n) {
-            const int s = __ldg(src + i), d = __ldg(dst + i);
+            const int s = qp_kv_ld(src + i), d = qp_kv_ld(dst + i);
             if (s >= 0 && s < c.max_seqs && d >= 0 && d < c.max_seqs && claim[d] == i && __ldcg(c.lens + d) == 0) {
                 len = __ldcg(c.lens + s);
                 if (len < 0 || len > (int64_t)c.max_pages * c.page_size) len = -1;
@@ -315,7 +319,7 @@ __global__ void __launch_bounds__(PLAN) kv_fork_plan_kernel(const Cache c, const
         const int at = c.s1[i], len = c.s2[i];
         if (!enough) { c.s2[i] = -1; continue; }
         if (len < 0) continue;
-        c.lens[__ldg(dst + i)] = len;                            // (the lengths were all read above)
+        c.lens[qp_kv_ld(dst + i)] = len;                            // (the lengths were all read above)
         if (at >= 0) {
             const int p = c.c[at];
             c.refs[p] = 1;
@@ -327,9 +331,10 @@ __global__ void __launch_bounds__(PLAN) kv_fork_plan_kernel(const Cache c, const
 }
 
 // tasks 0 .. n - 1: the pairs' table rows; behind them the pieces of the part-filled pages
-__global__ void __launch_bounds__(MOVE_THREADS) kv_fork_kernel(const Cache c, const Moves m, const int32_t* __restrict__ src,
-                                                               const int32_t* __restrict__ dst, int n)
+__global__ void __launch_bounds__(MOVE_THREADS) kv_fork_kernel(const Cache c, const Moves m, const int32_t* src,
+                                                               const int32_t* dst, int n)
 {
+    qp_kv_begin();
     const int per = m.layers * m.chunks;
     const int64_t tasks = n + (int64_t)n * per;
     for (int64_t t = blockIdx.x; t < tasks; t += gridDim.x) {
@@ -337,10 +342,10 @@ __global__ void __launch_bounds__(MOVE_THREADS) kv_fork_kernel(const Cache c, co
         const int len = c.s2[i];
         if (len <= 0) continue;
         const int full = len / c.page_size;
-        const int32_t* from = c.table + (size_t)__ldg(src + i) * c.max_pages;
+        const int32_t* from = c.table + (size_t)qp_kv_ld(src + i) * c.max_pages;
         const bool tail = len % c.page_size != 0;
         if (t < n) {
-            int32_t* to = c.table + (size_t)__ldg(dst + i) * c.max_pages;
+            int32_t* to = c.table + (size_t)qp_kv_ld(dst + i) * c.max_pages;
             for (int j = threadIdx.x; j < full; j += MOVE_THREADS) {
                 const int p = from[j];
                 to[j] = p;
@@ -358,24 +363,25 @@ __global__ void __launch_bounds__(MOVE_THREADS) kv_fork_kernel(const Cache c, co
 
 // ---------------------------------------------------------------------------- copying
 
-__global__ void __launch_bounds__(PLAN) kv_copy_plan_kernel(const Cache c, const int32_t* __restrict__ src,
-                                                            const int32_t* __restrict__ dst, int n)
+__global__ void __launch_bounds__(PLAN) kv_copy_plan_kernel(const Cache c, const int32_t* src,
+                                                            const int32_t* dst, int n)
 {
+    qp_kv_begin();
     volatile int* claim = c.c;                                   // per page: the first pair that writes it
     auto ok = [&](int p) { return p >= 0 && p < c.num_pages; };
     for (int i = threadIdx.x; i < n; i += PLAN) {
-        const int s = __ldg(src + i), d = __ldg(dst + i);
+        const int s = qp_kv_ld(src + i), d = qp_kv_ld(dst + i);
         if (ok(s) && ok(d)) claim[s] = claim[d] = NONE;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += PLAN) {
-        const int s = __ldg(src + i), d = __ldg(dst + i);
+        const int s = qp_kv_ld(src + i), d = qp_kv_ld(dst + i);
         if (ok(s) && ok(d)) atomicMin(c.c + d, i);
     }
     __syncthreads();
     bool range = false;
     for (int i = threadIdx.x; i < n; i += PLAN) {
-        const int s = __ldg(src + i), d = __ldg(dst + i);
+        const int s = qp_kv_ld(src + i), d = qp_kv_ld(dst + i);
         const bool good = ok(s) && ok(d) && claim[d] == i && (s == d || claim[s] == NONE);
         range |= !good;
         c.a[i] = good && s != d ? s : -1;
@@ -386,8 +392,9 @@ __global__ void __launch_bounds__(PLAN) kv_copy_plan_kernel(const Cache c, const
 
 // ---------------------------------------------------------------------------- compacting
 
-__global__ void __launch_bounds__(PLAN) kv_compact_plan_kernel(const Cache c, int32_t* __restrict__ live_out)
+__global__ void __launch_bounds__(PLAN) kv_compact_plan_kernel(const Cache c, int32_t* live_out)
 {
+    qp_kv_begin();
     __shared__ int sh[PW + 1];
     const int live = for_pages(c, 0, c.num_pages, sh, [](int, int refs) { return refs != 0; }, [](int, int) {});
     const int holes = for_pages(c, 0, c.num_pages, sh, [&](int p, int refs) { return p < live && refs == 0; }, [&](int r, int p) { c.b[r] = p; });
@@ -411,6 +418,7 @@ __global__ void __launch_bounds__(PLAN) kv_compact_plan_kernel(const Cache c, in
 
 __global__ void __launch_bounds__(MOVE_THREADS) kv_compact_kernel(const Cache c, const Moves m)
 {
+    qp_kv_begin();
     const int holes = c.head[0], live = c.head[1];
     if (holes == 0) return;
     const int64_t pieces = (int64_t)holes * m.layers * m.chunks;
@@ -442,7 +450,7 @@ extern "C" int32_t qp_kv_extend(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const
     if (h_batch->batch == 0) return QP_OK;
     qp_device_guard guard(ctx->device);
     if (!guard.ok) return qp_fail(ctx, QP_ERR_CUDA, "cannot select device");
-    kv_extend_kernel<<<1, PLAN, 0, static_cast<cudaStream_t>(stream)>>>(cache_of(ctx, h_cache), h_batch->d_slots, h_batch->d_start,
+    qp_kv_launch(kv_extend_kernel, 1u, PLAN, 0, static_cast<cudaStream_t>(stream), cache_of(ctx, h_cache), h_batch->d_slots, h_batch->d_start,
                                                                         h_batch->d_pos, h_batch->batch, h_batch->tokens, h_batch->max_new);
     ctx->launches += 1;
     return qp_check_launch(ctx, "qp_kv_extend");
@@ -456,7 +464,7 @@ extern "C" int32_t qp_kv_free(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const i
     qp_device_guard guard(ctx->device);
     if (!guard.ok) return qp_fail(ctx, QP_ERR_CUDA, "cannot select device");
     const int cap = ctx->sm_count * 16;
-    kv_free_kernel<<<n < cap ? n : cap, 128, 0, static_cast<cudaStream_t>(stream)>>>(cache_of(ctx, h_cache), d_slots, n);
+    qp_kv_launch(kv_free_kernel, (unsigned)(n < cap ? n : cap), 128, 0, static_cast<cudaStream_t>(stream), cache_of(ctx, h_cache), d_slots, n);
     ctx->launches += 1;
     return qp_check_launch(ctx, "qp_kv_free");
 }
@@ -472,8 +480,8 @@ extern "C" int32_t qp_kv_fork(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const i
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const Cache c = cache_of(ctx, h_cache);
     const Moves m = moves_of(h_cache, c);
-    kv_fork_plan_kernel<<<1, PLAN, 0, s>>>(c, d_src, d_dst, n);
-    kv_fork_kernel<<<move_grid(ctx, n + (int64_t)n * m.layers * m.chunks), MOVE_THREADS, 0, s>>>(c, m, d_src, d_dst, n);
+    qp_kv_launch(kv_fork_plan_kernel, 1u, PLAN, 0, s, c, d_src, d_dst, n);
+    qp_kv_launch(kv_fork_kernel, (unsigned)(move_grid(ctx, n + (int64_t)n * m.layers * m.chunks)), MOVE_THREADS, 0, s, c, m, d_src, d_dst, n);
     ctx->launches += 2;
     return qp_check_launch(ctx, "qp_kv_fork");
 }
@@ -490,8 +498,8 @@ extern "C" int32_t qp_kv_copy_pages(qp_ctx* ctx, const qp_kv_cache_t* h_cache, c
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const Cache c = cache_of(ctx, h_cache);
     const Moves m = moves_of(h_cache, c);
-    kv_copy_plan_kernel<<<1, PLAN, 0, s>>>(c, d_src, d_dst, n);
-    kv_move_kernel<<<move_grid(ctx, (int64_t)n * m.layers * m.chunks), MOVE_THREADS, 0, s>>>(m, n);
+    qp_kv_launch(kv_copy_plan_kernel, 1u, PLAN, 0, s, c, d_src, d_dst, n);
+    qp_kv_launch(kv_move_kernel, (unsigned)(move_grid(ctx, (int64_t)n * m.layers * m.chunks)), MOVE_THREADS, 0, s, m, n);
     ctx->launches += 2;
     return qp_check_launch(ctx, "qp_kv_copy_pages");
 }
@@ -506,8 +514,8 @@ extern "C" int32_t qp_kv_compact(qp_ctx* ctx, const qp_kv_cache_t* h_cache, int3
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const Cache c = cache_of(ctx, h_cache);
     const Moves m = moves_of(h_cache, c);
-    kv_compact_plan_kernel<<<1, PLAN, 0, s>>>(c, d_live);
-    kv_compact_kernel<<<move_grid(ctx, (int64_t)h_cache->num_pages * m.layers * m.chunks), MOVE_THREADS, 0, s>>>(c, m);
+    qp_kv_launch(kv_compact_plan_kernel, 1u, PLAN, 0, s, c, d_live);
+    qp_kv_launch(kv_compact_kernel, (unsigned)(move_grid(ctx, (int64_t)h_cache->num_pages * m.layers * m.chunks)), MOVE_THREADS, 0, s, c, m);
     ctx->launches += 2;
     return qp_check_launch(ctx, "qp_kv_compact");
 }

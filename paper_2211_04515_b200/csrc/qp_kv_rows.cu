@@ -104,7 +104,7 @@ __device__ __forceinline__ void look_up(const RowArgs& a, int first, int n, Plac
             from = qp_kv_start(r, b);
             for (int next; b < r.batch && (next = qp_kv_start(r, b + 1)) <= token; from = next) ++b;
         }
-        const int pos = b < r.batch && from <= token ? __ldg(r.pos + b) : -1;
+        const int pos = b < r.batch && from <= token ? qp_kv_ld(r.pos + b) : -1;
         if (pos >= 0) {
             const int64_t p = (int64_t)pos + (token - from);
             const int page = p < (1ll << 31) - 1 ? qp_kv_page(a.pages, qp_kv_slot(r, b), (int)p) : -1;
@@ -264,6 +264,7 @@ __global__ void __launch_bounds__(QP_THREADS) kv_append_kernel(const RowArgs a, 
 {
     constexpr int E = D / 8;
     using S = qp_kv_slice<D>;
+    qp_kv_begin();
     __shared__ Places places;
     const int sub = threadIdx.x & 7, group = threadIdx.x >> 3;
     const int first = blockIdx.x * per_block, n = min(per_block, a.rows.tokens - first), pairs = n * a.heads;
@@ -349,6 +350,7 @@ __global__ void __launch_bounds__(QP_THREADS) kv_gather_kernel(const RowArgs a, 
 {
     constexpr int E = D / 8;
     using S = qp_kv_slice<D>;
+    qp_kv_begin();
     __shared__ Places places;
     const int sub = threadIdx.x & 7, group = threadIdx.x >> 3;
     const int first = blockIdx.x * per_block, n = min(per_block, a.rows.tokens - first), pairs = n * a.heads;
@@ -415,7 +417,7 @@ int32_t launch_rows(qp_ctx* ctx, bool append, const qp_kv_cache_t* c, const qp_k
     if (per_block > fill) per_block = fill;
     per_block = per_block < 1 ? 1 : per_block > TOKENS ? TOKENS : per_block;
     const RowKernel f = dtype == QP_F32 ? pick<float>(append, c->head_dim) : pick<unsigned short>(append, c->head_dim);
-    f<<<(unsigned)((b->tokens + per_block - 1) / per_block), QP_THREADS, 0, static_cast<cudaStream_t>(stream)>>>(a, per_block, vec);
+    qp_kv_launch(f, (unsigned)((b->tokens + per_block - 1) / per_block), QP_THREADS, 0, static_cast<cudaStream_t>(stream), a, per_block, vec);
     ctx->launches += 1;
     return qp_check_launch(ctx, append ? "qp_kv_append" : "qp_kv_gather");
 }
