@@ -291,16 +291,23 @@ __device__ __forceinline__ void put_out(unsigned short* p, bool vec, const float
         for (int i = 0; i < 4; ++i) p[i] = h[i];
 }
 
-// four elements of query row r of a sequence, from their weighted sum and the weights' sum l about the reference m
-template <typename T, int D>
-__device__ __forceinline__ void put_row(const qp_kv_attn_args& a, const Seq& q, int head, int r, int d, float4 o, float m, float l)
+// What a tile's rows need at the end, worked out once by a thread each: where a row of out begins, and 1 over the sum of its weights (0 for
+// a row that saw nothing; NaN stays NaN).  Writes lse.
+struct RowEnds { int64_t at[16]; float over[16]; };
+template <typename T>
+__device__ __forceinline__ void end_row(const qp_kv_attn_args& a, const Seq& q, int head, int r, float m, float l, int64_t& at, float& over)
 {
     const int token = q.row0 + r / a.group, h = head * a.group + r % a.group;
-    const float f = l == 0.f ? 0.f : 1.f;                        // (NaN stays NaN)
-    const float v[4] = {f == 0.f ? 0.f : o.x / l, f == 0.f ? 0.f : o.y / l, f == 0.f ? 0.f : o.z / l, f == 0.f ? 0.f : o.w / l};
-    put_out(static_cast<T*>(a.out) + (int64_t)token * a.ot + (int64_t)h * a.oh + d, a.out_vec, v);
-    if (a.lse && d == 0)
-        a.lse[(int64_t)token * a.q_heads + h] = l == 0.f ? -__int_as_float(0x7F800000) : (m + log2f(l)) * 0.6931471805599453f;
+    at = (int64_t)token * a.ot + (int64_t)h * a.oh;
+    over = l == 0.f ? 0.f : 1.f / l;
+    if (a.lse) a.lse[(int64_t)token * a.q_heads + h] = l == 0.f ? -__int_as_float(0x7F800000) : (m + log2f(l)) * 0.6931471805599453f;
+}
+// four elements of a row, from their weighted sum
+template <typename T>
+__device__ __forceinline__ void put_row(const qp_kv_attn_args& a, int64_t at, float over, int d, float4 o)
+{
+    const float v[4] = {o.x * over, o.y * over, o.z * over, o.w * over};
+    put_out(static_cast<T*>(a.out) + at + d, a.out_vec, v);
 }
 
 // Whether this block is the last of n to come here (the counter is at zero again then).  What the others wrote before is visible.
@@ -321,7 +328,7 @@ __device__ __forceinline__ bool arrived(unsigned* count, int n, int& sh)
 // result again (it may be the first), or (null) into out.
 template <typename T, int D, int ROWS>
 __device__ __forceinline__ void add_parts(const qp_kv_attn_args& a, const Seq& q, int head, int tile, int rows, int at, int even,
-                                          int step, int n, float* sum, char* smem)
+                                          int step, int n, float* sum, char* smem, RowEnds& ends)
 {
     constexpr int PART = ROWS * (D + 2);
     auto part = [&](int i) { return a.part + (int64_t)(i ? even + 2 * step * i : at) * PART; };
@@ -341,6 +348,7 @@ __device__ __forceinline__ void add_parts(const qp_kv_attn_args& a, const Seq& q
         }
         tops[r] = top;
         tops[ROWS + r] = l;
+        if (!sum) end_row<T>(a, q, head, tile * ROWS + r, top, l, ends.at[r], ends.over[r]);
     }
     __syncthreads();
     // all of a thread's elements of some parts are asked for at once: what this costs is the trips to L2
@@ -375,7 +383,7 @@ __device__ __forceinline__ void add_parts(const qp_kv_attn_args& a, const Seq& q
         const int i = threadIdx.x + k * THREADS, r = i / (D / 4), d = 4 * (i % (D / 4));
         if (r >= rows) continue;
         if (!sum) {
-            put_row<T, D>(a, q, head, tile * ROWS + r, d, so[k], tops[r], tops[ROWS + r]);
+            put_row<T>(a, ends.at[r], ends.over[r], d, so[k]);
         } else {
             __stcg(reinterpret_cast<float4*>(sum + r * D + d), so[k]);
             if (d == 0) { __stcg(sum + ROWS * D + r, tops[r]); __stcg(sum + ROWS * D + ROWS + r, tops[ROWS + r]); }
@@ -399,6 +407,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     __shared__ Part part[2];
     __shared__ int sh_ok[WARPS][STAGES], sh_hi[WARPS][ROWS];    // slices that are there; last key that a query sees
     __shared__ int sh_last;
+    __shared__ RowEnds ends;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = lane >> 2, j = lane & 3;
 
     int b0 = 0;
@@ -798,26 +807,32 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             at = 2 * (int)blockIdx.x + (p.u == begin ? 0 : 1);
         }
         float* mine_at = a.part + (int64_t)at * C::PART;
-        for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
-            const int r = i / (D / 4), d = 4 * (i % (D / 4));
-            float top = mm[r];
+        if (threadIdx.x < (unsigned)rows) {                      // the warps' references become factors
+            const int r = threadIdx.x;
+            float top = mm[r], sl = 0.f;
 #pragma unroll
             for (int w = 1; w < WARPS; ++w) top = fmaxf(top, mm[w * ROWS + r]);
-            float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
-            float sl = 0.f;
 #pragma unroll
             for (int w = 0; w < WARPS; ++w) {
                 const float f = ex2(mm[w * ROWS + r] - top);
+                sl = fmaf(ml[w * ROWS + r], f, sl);
+                mm[w * ROWS + r] = f;
+            }
+            if (split) { __stcg(mine_at + ROWS * D + r, top); __stcg(mine_at + ROWS * D + ROWS + r, sl); }
+            else end_row<T>(a, q, head, tile * ROWS + r, top, sl, ends.at[r], ends.over[r]);
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < rows * (D / 4); i += THREADS) {
+            const int r = i / (D / 4), d = 4 * (i % (D / 4));
+            float4 so = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                const float f = mm[w * ROWS + r];
                 const float4 y = *reinterpret_cast<const float4*>(mo + (w * ROWS + r) * D + d);
                 so.x = fmaf(y.x, f, so.x); so.y = fmaf(y.y, f, so.y); so.z = fmaf(y.z, f, so.z); so.w = fmaf(y.w, f, so.w);
-                sl = fmaf(ml[w * ROWS + r], f, sl);
             }
-            if (!split) {
-                put_row<T, D>(a, q, head, tile * ROWS + r, d, so, top, sl);
-            } else {
-                __stcg(reinterpret_cast<float4*>(mine_at + r * D + d), so);
-                if (d == 0) { __stcg(mine_at + ROWS * D + r, top); __stcg(mine_at + ROWS * D + ROWS + r, sl); }
-            }
+            if (split) __stcg(reinterpret_cast<float4*>(mine_at + r * D + d), so);
+            else put_row<T>(a, ends.at[r], ends.over[r], d, so);
         }
         if (split) {
             // the parts of blocks c0 .. c1, `step` of them to a group; the group's sum takes the place of its first part
@@ -833,11 +848,11 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             float* sum = a.part + (int64_t)g_at * C::PART;
             bool mine = arrived(a.count + g_at, gn, sh_last);
             if (mine && groups == 1) {
-                add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, 1, parts, nullptr, smem);
+                add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, 1, parts, nullptr, smem, ends);
             } else if (mine) {
-                add_parts<T, D, ROWS>(a, q, head, tile, rows, g_at, 2 * gc, 1, gn, sum, smem);
+                add_parts<T, D, ROWS>(a, q, head, tile, rows, g_at, 2 * gc, 1, gn, sum, smem, ends);
                 mine = arrived(a.count + QP_KV_COUNTERS / 2 + first_at, groups, sh_last);
-                if (mine) add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, step, groups, nullptr, smem);
+                if (mine) add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, step, groups, nullptr, smem, ends);
             }
         }
         if (next >= end) break;
