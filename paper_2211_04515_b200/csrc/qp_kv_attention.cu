@@ -39,7 +39,12 @@ constexpr float M_NONE = -3.0e38f;               // reference before any score
 constexpr float M_SLACK = 8.f;                   // a score may pass the reference by this (log2)
 constexpr float V_SLACK = 64.f;                  // and a scale of V its norm by this: p * scale' <= 2^14 in fp16
 constexpr int UNIT = 4;                          // slices
-constexpr int HEAD = 6;                          // units
+// What an item's beginning and end cost, in units: 3 / 6 / 9 / 12 took 62.2 / 58.8 / 58.6 / 60.9 us for 64 sequences of 200 to 8191 tokens, 35.3 /
+// 33.0 / 32.2 / 33.7 for drafted tokens of 16 sequences, 19.0 / 18.2 / 19.4 / 20.1 for 24 short sequences in fp32.
+constexpr int HEAD = 6;
+// Units that are worth a block: 1 / 2 / 3 / 4 took 13.0 / 11.5 / 12.2 / 12.3 us for one sequence of 1021 tokens (16 parts to an item are
+// added in two levels, 8 in one); with more work than blocks there is no difference.
+constexpr int MIN_RUN = 2;
 constexpr int MANY = 64;                         // query rows to a cached head from which on the tensor-memory kernel is the faster
 
 template <int D, int NT, bool SPLIT> struct Cfg {
@@ -413,7 +418,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     int b0 = 0;
     int64_t base = 0, upto = load_chunk<ROWS>(a, 0, 0, chunk), W = upto;
     for (int c = THREADS; c < a.rows.batch; c += THREADS) W = load_chunk<ROWS>(a, c, W, chunk);
-    const int64_t blocks = (int64_t)gridDim.x < W ? (int64_t)gridDim.x : W;
+    const int64_t blocks = (int64_t)gridDim.x * MIN_RUN < W ? (int64_t)gridDim.x : (W + MIN_RUN - 1) / MIN_RUN;
     if ((int64_t)blockIdx.x >= blocks) return;
     const int64_t begin = quotient(blockIdx.x * W, blocks), end = quotient((blockIdx.x + 1ll) * W, blocks);
     if (a.rows.batch > THREADS) {                                // back to the chunk that the run begins in
