@@ -601,7 +601,7 @@ typedef struct {
 
 /* The new tokens of a step.  Sequence b of the batch is slot d_slots[b] (NULL: slot b); its tokens are the rows
  * d_start[b] .. d_start[b + 1] - 1 (NULL: row b alone) of the step's K, V and Q buffers, and the first of them has position
- * d_pos[b] in the sequence.  d_pos[b] < 0: the sequence takes no part.  tokens bounds the rows of the
+ * d_pos[b] in the sequence.  d_pos[b] < 0 (or so large that a position passes 2^31 - 1): the sequence takes no part.  tokens bounds the rows of the
  * buffers: rows behind d_start[batch] (or at and behind `tokens`) are neither read nor written.  max_new bounds the
  * tokens of one sequence; what a sequence has beyond them is skipped with QP_DEV_KV_RANGE by qp_kv_extend
  * (the whole sequence) and qp_kv_attention (the rows behind).  d_start ascends. */
@@ -647,6 +647,10 @@ int32_t qp_kv_gather(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batc
  * and sums are fp32; out has q's type.  d_lse (or NULL): [tokens, q_heads] fp32, the natural logarithm of the sum
  * of the exponentials.  A row that sees no key is 0 with lse -inf; a query with a non-finite element gives NaN in its row
  * only.  A token on a page that the table does not name counts as masked, with QP_DEV_KV_RANGE.
+ * Where a bf16 sequence has 160 or more query rows to a cached head (its tokens times q_heads / heads) and head_dim is 64 or
+ * 128, the values of K and V are rounded to fp16 (2^-11) on the way into the products, and so are the weights; otherwise
+ * only the weights are (fp32: neither, to 2^-22).  A wait inside that kernel which does not end within the limit of
+ * qp_set_wait_limit_for_testing raises QP_DEV_STREAM_TIMEOUT, as elsewhere.
  * The plan holds what stays from call to call; its workspace belongs to one stream at a time and is zeroed once,
  * before its first use (each call leaves its counters at zero). */
 typedef struct {

@@ -45,7 +45,10 @@ constexpr int HEAD = 6;
 // Units that are worth a block: 1 / 2 / 3 / 4 took 13.0 / 11.5 / 12.2 / 12.3 us for one sequence of 1021 tokens (16 parts to an item are
 // added in two levels, 8 in one); with more work than blocks there is no difference.
 constexpr int MIN_RUN = 2;
-constexpr int MANY = 64;                         // query rows to a cached head from which on the tensor-memory kernel is the faster
+// Query rows of a sequence to a cached head from which on the tensor-memory kernel takes it.  This one against that, us, at 64 / 128 / 256
+// rows: 35 / 55 / 94 against 55 / 58 / 67 for 4 sequences of 4000 tokens and 8 heads; at 128 rows 94 against 71 for 16 of 4000
+// and 4 heads, 53 against 92 for one of 16000.
+constexpr int MANY = 160;
 
 template <int D, int NT, bool SPLIT> struct Cfg {
     static constexpr int ROWS = 8 * NT;
@@ -150,7 +153,7 @@ struct Seq {
 template <int ROWS>
 __device__ __forceinline__ void derive(const qp_kv_attn_args& a, Seq& q)
 {
-    if (q.n <= 0 || q.pos < 0 || (int64_t)q.n * a.group >= a.many) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return; }
+    if (q.n <= 0 || q.pos < 0 || q.pos > 0x7FFFFFFF - q.n || (int64_t)q.n * a.group >= a.many) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return; }
     const unsigned most = (unsigned)a.pages.max_pages * (unsigned)a.pages.page_size;     // (below 2^31, as pos and n)
     const unsigned end0 = (unsigned)q.pos + (unsigned)q.n, end = end0 < most ? end0 : most;
     unsigned lo = a.window > 0 && q.pos >= a.window ? (unsigned)(q.pos - a.window + 1) : 0u;
@@ -171,7 +174,10 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
     q.row0 = qp_kv_start(a.rows, b);
     const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
     q.n = row1 - q.row0;
-    if (q.n > a.max_new) q.n = a.max_new;
+    if (q.n > a.max_new) {                                       // (every block comes here for every sequence; one says so)
+        if (blockIdx.x == 0) atomicOr(a.status, QP_DEV_KV_RANGE);
+        q.n = a.max_new;
+    }
     derive<ROWS>(a, q);
     return q;
 }

@@ -211,7 +211,7 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
     q.n = row1 - q.row0;
     if (q.n > a.max_new) q.n = a.max_new;
     const int64_t rows = (int64_t)q.n * a.group;
-    q.tiles = q.n <= 0 || q.pos < 0 || rows < a.many ? 0 : (int)((rows + ROWS - 1) / ROWS);
+    q.tiles = q.n <= 0 || q.pos < 0 || q.pos > 0x7FFFFFFF - q.n || rows < a.many ? 0 : (int)((rows + ROWS - 1) / ROWS);
     return q;
 }
 // slices [first, first + 8 * returned) hold the keys that rows tile * ROWS .. see (counts of rows and of keys fit 32 bits)

@@ -228,7 +228,7 @@ def test_rows_are_those_of_the_token_calls(ctx, dim, dtype):
 
 def halves(dtype, dim, rows):
     """Whether these query rows to a cached head go through the kernel that takes K and V in fp16."""
-    return dtype == BF16 and dim <= 128 and rows >= 64
+    return dtype == BF16 and dim <= 128 and rows >= 160
 
 
 def check_attention(ctx, cache, lens_k, slots, pos, start, q, window, got, lse, scale, rows_left=None):
@@ -698,6 +698,74 @@ def test_captured_step_replays(ctx):
         del graph
     for s in sides:
         s[0].close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [3, 60])
+def test_more_tokens_than_said(ctx, new):
+    """Rows beyond max_new are skipped and reported; rows at and behind `tokens` are left alone whatever start says."""
+    rng = np.random.default_rng(14)
+    lens, heads, group, dim = [200, 130], 1, 4, 64
+    cache = make(rng, lens, heads, dim, 16)
+    fill(ctx, rng, cache, lens)
+    q = torch.from_numpy(rng.standard_normal((2 * new + 4, group, dim)).astype(np.float32)).cuda().to(BF16)
+    pos, start = [200 - new - 2, 130 - new], [0, new + 2, 2 * new + 4]
+    plan = ctx.qp_kv_attention_plan(cache, group)
+    out, lse = torch.full_like(q, 5.0), torch.full((2 * new + 4, group), 5.0, device="cuda")
+    batch = qp.KVBatch(ints(pos), start=ints(start), tokens=2 * new + 1, max_new=new)
+    ctx.qp_kv_attention(cache, batch, q, plan, out=out, lse=lse)
+    assert ctx.qp_get_status() == qp.QP_DEV_KV_RANGE
+    check_attention(ctx, cache, lens, [0], pos[:1], [0, new], q, 0, out, lse, dim ** -0.5)
+    assert (out[new:new + 2] == 5).all() and (out[2 * new + 1:] == 5).all() and (lse[2 * new + 1:] == 5).all()
+    assert (out[new + 2:2 * new + 1] != 5).any()
+    ctx.qp_kv_append(cache, batch, q[:, :1].contiguous(), q[:, :1].contiguous())
+    k, _ = ctx.qp_kv_gather(cache, batch, q[:, :1].contiguous() * 0 + 5, q[:, 1:2].contiguous())
+    assert (k[2 * new + 1:] == 5).all() and ctx.qp_get_status() == 0
+
+
+@pytest.mark.gpu
+def test_calls_follow_each_other(ctx):
+    """Each call is set up while the one before it runs: chains of dependent calls without a wait between, on a stream of their own, after
+    and before kernels of other kinds, give what the same calls give with a wait between."""
+    rng = np.random.default_rng(15)
+    heads, group, dim, page = 4, 2, 128, 16
+    results = []
+    for waits in (True, False):
+        gen = torch.Generator(device="cuda")
+        gen.manual_seed(3)
+        cache = qp.KVCache.empty(400, heads, dim, 24, 30, page, 2)
+        cache.pool.zero_()
+        plan = ctx.qp_kv_attention_plan(cache, heads * group)
+        outs = []
+        stream = torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        pause = stream.synchronize if waits else (lambda: None)
+        with torch.cuda.stream(stream):
+            for step in range(25):
+                n = 8 if step % 5 else 24
+                new = 40 if step == 0 else 1
+                start = torch.arange(0, (n + 1) * new, new, dtype=torch.int32, device="cuda")
+                batch = qp.KVBatch(torch.zeros(n, dtype=torch.int32, device="cuda"), start=start, tokens=n * new, max_new=new)
+                k, v = torch.randn(2, n * new, heads, dim, device="cuda", generator=gen).to(BF16)
+                q = torch.randn(n * new, heads * group, dim, device="cuda", generator=gen).to(BF16)
+                ctx.qp_kv_extend(cache, batch), pause()
+                for layer in range(2):
+                    ctx.qp_kv_append(cache, batch, k, v + layer, layer), pause()
+                    out = ctx.qp_kv_attention(cache, batch, q, plan, layer)
+                    pause()
+                    outs.append(out * 2)
+                    q = out + q
+                if step % 7 == 3:
+                    ctx.qp_kv_free(cache, ints([1, 5, 20])), pause()
+                    ctx.qp_kv_fork(cache, ints([0, 2, 2]), ints([1, 5, 20])), pause()
+                    ctx.qp_kv_compact(cache), pause()
+        stream.synchronize()
+        assert ctx.qp_get_status() == 0
+        results.append((outs, cache))
+    for a, b in zip(*(r[0] for r in results)):
+        assert torch.equal(a, b)
+    a, b = (r[1] for r in results)
+    assert a.lens.tolist() == b.lens.tolist() and torch.equal(a.table, b.table) and torch.equal(a.refs, b.refs)
 
 
 @pytest.mark.gpu
