@@ -363,11 +363,15 @@ __global__ void __launch_bounds__(MOVE_THREADS) kv_fork_kernel(const Cache c, co
 
 // ---------------------------------------------------------------------------- copying
 
+constexpr int SMEM_PAGES = 12288;                // pages whose claims fit shared memory
+
 __global__ void __launch_bounds__(PLAN) kv_copy_plan_kernel(const Cache c, const int32_t* src,
-                                                            const int32_t* dst, int n)
+                                                            const int32_t* dst, int n, bool in_shared)
 {
     qp_kv_begin();
-    volatile int* claim = c.c;                                   // per page: the first pair that writes it
+    extern __shared__ int sh_claims[];
+    int* list = in_shared ? sh_claims : c.c;                     // per page: the first pair that writes it
+    volatile int* claim = list;
     auto ok = [&](int p) { return p >= 0 && p < c.num_pages; };
     for (int i = threadIdx.x; i < n; i += PLAN) {
         const int s = qp_kv_ld(src + i), d = qp_kv_ld(dst + i);
@@ -376,7 +380,7 @@ __global__ void __launch_bounds__(PLAN) kv_copy_plan_kernel(const Cache c, const
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += PLAN) {
         const int s = qp_kv_ld(src + i), d = qp_kv_ld(dst + i);
-        if (ok(s) && ok(d)) atomicMin(c.c + d, i);
+        if (ok(s) && ok(d)) atomicMin(list + d, i);
     }
     __syncthreads();
     bool range = false;
@@ -395,7 +399,55 @@ __global__ void __launch_bounds__(PLAN) kv_copy_plan_kernel(const Cache c, const
 __global__ void __launch_bounds__(PLAN) kv_compact_plan_kernel(const Cache c, int32_t* live_out)
 {
     qp_kv_begin();
-    __shared__ int sh[PW + 1];
+    __shared__ int sh[PW + 1], sh_hole[PER * PLAN / 2];
+    if (c.num_pages <= PER * PLAN) {                             // every page in a register: the table is read once
+        const int lane = threadIdx.x & 31, p0 = (threadIdx.x >> 5) * 32 * PER + lane;
+        int refs[PER], n = 0, live, both;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) refs[i] = p0 + 32 * i < c.num_pages ? __ldcg(c.refs + p0 + 32 * i) : 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) n += __popc(__ballot_sync(0xFFFFFFFFu, refs[i] != 0));
+        block_scan(lane == 0 ? n : 0, sh, live);
+        unsigned holes[PER], movers[PER];
+        n = 0;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {                          // (at most 4096 of either: two sums to a word)
+            holes[i] = __ballot_sync(0xFFFFFFFFu, p0 + 32 * i < live && refs[i] == 0);
+            movers[i] = __ballot_sync(0xFFFFFFFFu, p0 + 32 * i >= live && refs[i] != 0);
+            n += __popc(holes[i]) + (__popc(movers[i]) << 16);
+        }
+        const int at = __shfl_sync(0xFFFFFFFFu, block_scan(lane == 0 ? n : 0, sh, both), 0);
+        const unsigned below = (1u << lane) - 1u;
+        int rank = at & 0xFFFF;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            if (holes[i] >> lane & 1u) sh_hole[rank + __popc(holes[i] & below)] = p0 + 32 * i;
+            rank += __popc(holes[i]);
+        }
+        __syncthreads();
+        rank = at >> 16;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int p = p0 + 32 * i;
+            if (movers[i] >> lane & 1u) {
+                const int k = rank + __popc(movers[i] & below), to = sh_hole[k];
+                c.a[k] = p;
+                c.b[k] = to;
+                c.c[p] = to;
+                c.refs[to] = refs[i];
+                c.refs[p] = 0;
+            } else if (p >= live && p < c.num_pages) {
+                c.c[p] = -1;
+            }
+            rank += __popc(movers[i]);
+        }
+        if (threadIdx.x == 0) {
+            c.head[0] = both & 0xFFFF;
+            c.head[1] = live;
+            if (live_out) *live_out = live;
+        }
+        return;
+    }
     const int live = for_pages(c, 0, c.num_pages, sh, [](int, int refs) { return refs != 0; }, [](int, int) {});
     const int holes = for_pages(c, 0, c.num_pages, sh, [&](int p, int refs) { return p < live && refs == 0; }, [&](int r, int p) { c.b[r] = p; });
     // every page at or above `live` has an entry in list c: where it goes, -1 for a free one
@@ -498,7 +550,8 @@ extern "C" int32_t qp_kv_copy_pages(qp_ctx* ctx, const qp_kv_cache_t* h_cache, c
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const Cache c = cache_of(ctx, h_cache);
     const Moves m = moves_of(h_cache, c);
-    qp_kv_launch(kv_copy_plan_kernel, 1u, PLAN, 0, s, c, d_src, d_dst, n);
+    const bool in_shared = h_cache->num_pages <= SMEM_PAGES;
+    qp_kv_launch(kv_copy_plan_kernel, 1u, PLAN, in_shared ? (size_t)h_cache->num_pages * 4 : 0, s, c, d_src, d_dst, n, in_shared);
     qp_kv_launch(kv_move_kernel, (unsigned)(move_grid(ctx, (int64_t)n * m.layers * m.chunks)), MOVE_THREADS, 0, s, m, n);
     ctx->launches += 2;
     return qp_check_launch(ctx, "qp_kv_copy_pages");
