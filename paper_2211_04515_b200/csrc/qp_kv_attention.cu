@@ -27,6 +27,11 @@
 //     subnormal's leading zeros are lost from the sum (1e-5 of the result), and it cuts sums off instead of rounding them.  So the codes
 //     are made normal numbers there, and less 8 while at it (lo is then the value of code 8: smaller sums), and each slice's
 //     sums start at zero and are added to the running ones by ordinary additions.
+//
+// Measured in a stream: 64 sequences of 200 to 8191 tokens, 32 query heads on 8 of 128: 59 us (212 MB, 3.6 TB/s over the whole call and 5.2
+// while codes are read; 49 % of the issue slots); 120001 and 131071 tokens, 64 query heads on 4: 57 us (143 MB, 2.5 TB/s: 16 queries to a
+// code); one sequence of 1021: 12 us; fp32, 24 sequences of 197 to 1500, 12 heads of 64: 18 us (15 MB).  A part of an item costs about 8 us beside
+// its codes, in latencies: its lengths and first codes 4, the reduction over warps 2, arrival and sum 2.
 #include "qp_kv.cuh"
 #include "qp_kv_attention.cuh"
 

@@ -10,6 +10,8 @@
 // bytes out, and by the instructions, about 12 to an element.  What keeps such a kernel from them is the chain of dependent loads batch -> position -> page -> row
 // (with the divisions between them 3 us, in every warp: 21 us for 8246 tokens of 8 heads), so one warp looks up a block's
 // tokens, a lane to a token, while the others' first rows are on their way.
+// Measured for 8246 tokens of 8 heads of 128 in bf16: append 20 us by itself (34 MB in, 10 out; 49 % of the issue slots), gather 13 (48 %), both in
+// a stream 30.
 #include "qp_kv.cuh"
 
 QP_CK_UNIT
