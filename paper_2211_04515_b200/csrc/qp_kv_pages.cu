@@ -153,9 +153,15 @@ __global__ void __launch_bounds__(PLAN) kv_extend_kernel(const Cache c, const in
             range |= old < 0;
         }
         int total;
+        // d_start need not ascend, so that many entries may ask for most of 2^31 tokens each: the sum is bounded first, without overflow
+        // (up to 2^23 tokens an entry 1024 of them want at most 2^29 + 2^10 pages)
+        if (max_new > 1 << 23) {                                 // uniform
+            block_scan(need >> 11, sh, total);
+            if (total > c.num_pages >> 11) { wanted = c.num_pages + 1; break; }
+        }
         const int at = wanted + block_scan(need, sh, total);
         if (b < batch) { c.s1[b] = at; c.s2[b] = old; }
-        wanted += total;                                         // (below 2^31: the claimed slots differ, and need is bounded by max_pages each)
+        wanted += total;                                         // (at most 2^29 before, 2^29 + 2^21 added)
         if (wanted > c.num_pages) break;                         // uniform
     }
     int* taken = wanted <= SMEM_TAKEN ? sh_taken : c.a;

@@ -588,6 +588,26 @@ def test_exhausted_pool_changes_nothing(ctx):
     assert ctx.qp_kv_extend(cache, batch).tolist() == [-1, -1] and ctx.qp_get_status() == qp.QP_DEV_KV_RANGE
 
 
+@pytest.mark.gpu
+def test_sums_of_pages_beyond_31_bits(ctx):
+    """17 of 33 sequences want 2^27 - 257 pages each, 2^31 + 2^27 - 4369 together, from starts that go up and down."""
+    most, n = 2**27 - 257, 33
+    i32 = dict(dtype=torch.int32, device="cuda:0")
+    pool = torch.empty(1, 4, 1, 1, qp.qp_kv_slice_bytes(64), dtype=torch.uint8, device="cuda:0")
+    cache = qp.KVCache(pool, torch.empty(n, most, **i32), torch.zeros(n, **i32), torch.zeros(4, **i32), 64)
+    tokens = 16 * most
+    batch = qp.KVBatch(torch.zeros(n, **i32), start=ints([0, tokens] * 17), tokens=tokens, max_new=tokens)
+    assert ctx.qp_kv_extend(cache, batch).tolist() == [-1] * n
+    assert ctx.qp_get_status() & qp.QP_DEV_KV_EXHAUSTED
+    assert cache.lens.tolist() == [0] * n and cache.refs.tolist() == [0] * 4
+    batch = qp.KVBatch(torch.zeros(n, **i32), start=ints([0] * 5 + [40] * 29), tokens=tokens, max_new=tokens)
+    assert ctx.qp_kv_extend(cache, batch).tolist() == [0] * n and ctx.qp_get_status() == 0
+    assert cache.lens.tolist() == [0] * 4 + [40] + [0] * 28 and cache.refs.tolist() == [1, 1, 1, 0]
+    assert cache.table[4, :3].tolist() == [0, 1, 2]
+    del cache
+    torch.cuda.empty_cache()
+
+
 def dense(ks, vs, q, dim, group):
     """Attention of q [q_heads, dim] over the fp64 rows ks, vs [heads, n, dim]."""
     out = []
