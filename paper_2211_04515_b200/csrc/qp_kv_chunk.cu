@@ -26,7 +26,7 @@
 //   - Registers: 128 a thread at launch; the softmax warps go to 160 (a row's 64 scores stay in registers), the issuing warp's group
 //     to 64 (2 * 160 + 128 + 64 = 4 * 128).  One copy of each hot loop: unrolled for each role they did not fit the instruction
 //     cache (1161 us against 936 for the case below).
-//   - Measured: 2048 tokens over 9001 and 16384, 32 query heads on 8 of 128: 838 us in short runs, 836 TFLOP/s, 939 with the GPU at its
+//   - Measured: 2048 tokens over 9001 and 16384, 32 query heads on 8 of 128: 838 us in short runs, 836 TFLOP/s, 935 with the GPU at its
 //     power limit.  52 % of the issue slots, tcgen05 44 % of the time.
 //   - Every wait has a limit: a block that gives up raises QP_DEV_STREAM_TIMEOUT, its roles leave, the products in flight are
 //     waited for, tensor memory is freed.

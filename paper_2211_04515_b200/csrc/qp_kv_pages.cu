@@ -5,7 +5,7 @@
 // These tables are small (a pool of 8192 pages has 32 KB of refs) and one block reads them in a few round trips, which
 // is what the call costs: 3 to 5 us.  A second launch over the whole GPU then moves the bytes, where there are any:
 // 16 bytes a thread, eight loads in flight, bound by HBM at 2 bytes per byte copied.  1001 pages of 73728 bytes in 2 layers: 50.9 us,
-// 43.6 of them the move (6.8 TB/s); compacting 4096 pages, 2 layers: 35.6, 25.5 of them the move.
+// 43.6 of them the move (6.8 TB/s); compacting 4096 pages, 2 layers: 35.3, 25.5 of them the move.
 #include "qp_kv.cuh"
 
 QP_CK_UNIT
