@@ -16,7 +16,9 @@
 //   - A warp takes slices of 16 tokens by itself: a ring of its own in shared memory, filled with 16-byte asynchronous
 //     copies (a slice is contiguous), no barrier with other warps until its part of the sequence ends.
 //   - Softmax with a reference instead of the running maximum: p = 2^(s - m) where m is only raised, by a vote, once a score
-//     passes it by 8; the same for the scale of V, so that p * scale' fits fp16.
+//     passes it by 6.  The weights p * scale' have a norm of their own for each query, lowered where one of them would leave fp16 and then
+//     so that the largest is at 2^7 or more: what fp16 drops (2^-25) is 2^-32 of the query's largest weight, and keys that it does not see,
+//     or whose p is next to nothing, have no part in it however large their values are.
 //   - The work of the whole batch, in units of 64 tokens of one item (sequence, head, tile of queries), is cut into equal runs, one
 //     for each resident block, whatever the lengths; an item counts HEAD units more than it has, for what its beginning and end
 //     cost.  Where a cut falls inside an item, its blocks leave partial results, and the last to finish (counters; nobody
@@ -41,8 +43,11 @@ namespace {
 
 constexpr int WARPS = 4, THREADS = WARPS * 32;
 constexpr float M_NONE = -3.0e38f;               // reference before any score
-constexpr float M_SLACK = 8.f;                   // a score may pass the reference by this (log2)
-constexpr float V_SLACK = 64.f;                  // and a scale of V its norm by this: p * scale' <= 2^14 in fp16
+constexpr float M_SLACK = 6.f;                   // a score may pass the reference by this (log2), so p is at most 64;
+constexpr float W_MOST = 64000.f;                // and p * scale' * norm at most this, in fp16; no need to look at p while
+constexpr float V_MOST = 1000.f;                 // scale' * norm is at most this
+constexpr float W_TOP = 256.f;                   // a norm that is lowered takes the largest weight to half of this or more
+constexpr float NORM_MOST = 8.507059e37f;        // 2^126: the norm before any weight
 constexpr int UNIT = 4;                          // slices
 // What an item's beginning and end cost, in units: 3 / 6 / 9 / 12 took 62.2 / 58.8 / 58.6 / 60.9 us for 64 sequences of 200 to 8191 tokens, 35.3 /
 // 33.0 / 32.2 / 33.7 for drafted tokens of 16 sequences, 19.0 / 18.2 / 19.4 / 20.1 for 24 short sequences in fp32.
@@ -566,8 +571,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         const int all_lo = a.window > 0 ? q.pos + last_i - a.window + 1 : 0;
 
         float o[NT][4 * VW][4];
-        qp_f2 mn[NT], l[NT], lv[NT];                             // the reference, negated; sums of p and of p * lo'
-        float vn = 1.2676506e30f;                                // 2^100
+        qp_f2 mn[NT], l[NT], lv[NT], wn[NT];                     // the reference, negated; sums of p and of p * lo'; norm of the weights
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -576,6 +580,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                 for (int c = 0; c < 4; ++c) o[t][i][c] = 0.f;
             mn[t] = qp_pack2(-M_NONE, -M_NONE);
             l[t] = lv[t] = qp_pack2(0.f, 0.f);
+            wn[t] = qp_pack2(NORM_MOST, NORM_MOST);
         }
 
         for (int it = 0; it < count; ++it) {
@@ -662,7 +667,13 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                             s[i][t][h] = qp_pack2(y[0], y[1]);
                         }
             }
-            float over = -1.f, vmax = 0.f;                       // how far the scores pass their references, the scales their norm
+            float over = -1.f, vmax = 0.f, nmax = 0.f;           // how far the scores pass their references; the largest scale of V and norm
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                float y0, y1;
+                qp_unpack2(wn[t], y0, y1);
+                nmax = qp_max3(nmax, y0, y1);
+            }
 #pragma unroll
             for (int i = 0; i < SL; ++i)
 #pragma unroll
@@ -675,64 +686,88 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                         over = qp_max3(over, y0, y1);
                     }
                 }
-            if (__any_sync(0xFFFFFFFFu, over > M_SLACK || vmax * vn > V_SLACK)) {      // rare: new references
+            if (__any_sync(0xFFFFFFFFu, over > M_SLACK || vmax * nmax > V_MOST)) {     // uncommon: look at the weights themselves
+                float most = 0.f;
 #pragma unroll
-                for (int o2 = 4; o2 < 32; o2 <<= 1) vmax = fmaxf(vmax, __shfl_xor_sync(0xFFFFFFFFu, vmax, o2));
-                float back = 1.f;
-                if (vmax * vn > V_SLACK) {
-                    int ex = 258 - (int)(__float_as_uint(vmax) >> 23);
-                    ex = ex > 254 ? 254 : ex;                    // (at least 258 - 254)
-                    const float next = __uint_as_float((unsigned)ex << 23);   // vmax * next in [16, 32)
-                    back = next / vn;
-                    vn = next;
-                }
+                for (int i = 0; i < SL; ++i)
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    float top[2] = {M_NONE, M_NONE}, old[2], f[2];
-                    qp_unpack2(mn[t], old[0], old[1]);
-#pragma unroll
-                    for (int i = 0; i < SL; ++i)
+                    for (int t = 0; t < NT; ++t)
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            float y0, y1;
-                            qp_unpack2(s[i][t][h], y0, y1);
-                            top[0] = fmaxf(top[0], y0);
-                            top[1] = fmaxf(top[1], y1);
+                            float y0, y1, n0, n1;
+                            qp_unpack2(qp_add2(s[i][t][h], mn[t]), y0, y1);
+                            qp_unpack2(wn[t], n0, n1);
+                            most = qp_max3(most, ex2(y0) * vq[i][h].y * n0, ex2(y1) * vq[i][h].y * n1);
                         }
+                if (__any_sync(0xFFFFFFFFu, over > M_SLACK || most > W_MOST)) {        // rare: new references
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) {
+                    for (int t = 0; t < NT; ++t) {
+                        float top[2] = {M_NONE, M_NONE}, w[2] = {0.f, 0.f}, old[2], norm[2], f[2], back[2];
+                        qp_unpack2(mn[t], old[0], old[1]);
+                        qp_unpack2(wn[t], norm[0], norm[1]);
 #pragma unroll
-                        for (int o2 = 4; o2 < 32; o2 <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xFFFFFFFFu, top[c], o2));
-                        top[c] = fmaxf(-old[c], top[c]);
-                        f[c] = ex2(-old[c] - top[c]);
+                        for (int i = 0; i < SL; ++i)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float y0, y1;
+                                qp_unpack2(s[i][t][h], y0, y1);
+                                top[0] = fmaxf(top[0], y0);
+                                top[1] = fmaxf(top[1], y1);
+                            }
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                            for (int o2 = 4; o2 < 32; o2 <<= 1) top[c] = fmaxf(top[c], __shfl_xor_sync(0xFFFFFFFFu, top[c], o2));
+                            top[c] = fmaxf(-old[c], top[c]);
+                            f[c] = ex2(-old[c] - top[c]);
+                        }
+                        mn[t] = qp_pack2(-top[0], -top[1]);
+#pragma unroll
+                        for (int i = 0; i < SL; ++i)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                float y0, y1;
+                                qp_unpack2(s[i][t][h], y0, y1);
+                                w[0] = fmaxf(w[0], ex2(y0 - top[0]) * vq[i][h].y);
+                                w[1] = fmaxf(w[1], ex2(y1 - top[1]) * vq[i][h].y);
+                            }
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                            for (int o2 = 4; o2 < 32; o2 <<= 1) w[c] = fmaxf(w[c], __shfl_xor_sync(0xFFFFFFFFu, w[c], o2));
+                            // the p so far are f times as large: the norm takes that up where it can, so that what out holds may stay
+                            float next = f[c] > 0.f ? fminf(norm[c] / f[c], NORM_MOST) : NORM_MOST;
+                            if (w[c] * next > W_TOP) {
+                                const int ex = 261 - (int)(__float_as_uint(w[c]) >> 23);          // w * next in [2^7, 2^8)
+                                next = __uint_as_float((unsigned)(ex > 253 ? 253 : ex < 1 ? 1 : ex) << 23);
+                            }
+                            back[c] = f[c] > 0.f ? f[c] * (next / norm[c]) : 0.f;
+                            norm[c] = next;
+                        }
+                        wn[t] = qp_pack2(norm[0], norm[1]);
+                        l[t] = mul2(l[t], qp_pack2(f[0], f[1]));
+                        lv[t] = mul2(lv[t], qp_pack2(f[0], f[1]));
+#pragma unroll
+                        for (int i = 0; i < 4 * VW; ++i)
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) o[t][i][c] *= back[c & 1];
                     }
-                    mn[t] = qp_pack2(-top[0], -top[1]);
-                    l[t] = mul2(l[t], qp_pack2(f[0], f[1]));
-                    lv[t] = mul2(lv[t], qp_pack2(f[0], f[1]));
-                    f[0] *= back;
-                    f[1] *= back;
-#pragma unroll
-                    for (int i = 0; i < 4 * VW; ++i)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) o[t][i][c] *= f[c & 1];
                 }
             }
 #pragma unroll
             for (int i = 0; i < SL; ++i) {
-                // probabilities; times V's scale they are the second product's operand
+                // probabilities; times V's scale and the norm they are the second product's operand
                 unsigned pb[NT][2], pl[SPLIT ? NT : 1][2];
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        float p0, p1;
+                        float p0, p1, w0, w1;
                         qp_unpack2(qp_add2(s[i][t][h], mn[t]), p0, p1);
                         const qp_f2 p = qp_pack2(ex2(p0), ex2(p1));
                         l[t] = qp_add2(l[t], p);
                         lv[t] = qp_fma2(p, qp_pack2(vq[i][h].x, vq[i][h].x), lv[t]);
-                        const float vs = vq[i][h].y * vn;
-                        float w0, w1;
-                        qp_unpack2(mul2(p, qp_pack2(vs, vs)), w0, w1);
+                        qp_unpack2(mul2(mul2(p, qp_pack2(vq[i][h].y, vq[i][h].y)), wn[t]), w0, w1);
                         const unsigned x2 = half2_of(w0, w1);
                         pb[t][h] = transpose8(x2);
                         if constexpr (SPLIT) pl[t][h] = transpose8(half2_of(w0 - half_lo(x2), w1 - half_hi(x2)));
@@ -786,10 +821,10 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         float* mo = reinterpret_cast<float*>(smem);
         float* mm = mo + WARPS * ROWS * D;
         float* ml = mm + WARPS * ROWS;
-        const float un = 1.f / vn;
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            float sl[2], sv[2], mc[2];
+            float sl[2], sv[2], mc[2], norm0, norm1;
+            qp_unpack2(wn[t], norm0, norm1);
             qp_unpack2(l[t], sl[0], sl[1]);
             qp_unpack2(lv[t], sv[0], sv[1]);
             qp_unpack2(mn[t], mc[0], mc[1]);
@@ -803,9 +838,11 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                 const int r = 8 * t + 2 * j + c;
                 if (n == 0) { mm[warp * ROWS + r] = -mc[c]; ml[warp * ROWS + r] = sl[c]; }
                 float* row = mo + (warp * ROWS + r) * D + n * (D / 8);
+                // (codes as subnormals: 2^24 in two steps, so that neither leaves fp32)
+                constexpr float f = SPLIT ? 1.f : 4096.f, less = SPLIT ? 0.f : 1.f;
+                const float un = f / (c ? norm1 : norm0);
 #pragma unroll
                 for (int i = 0; i < 4 * VW; i += 2) {            // tiles i and i + 1: elements e, e + 2 and e + 1, e + 3 of word i / 4
-                    constexpr float f = SPLIT ? 1.f : 16777216.f, less = SPLIT ? 0.f : 1.f;
                     *reinterpret_cast<float4*>(row + 8 * (i >> 2) + 4 * ((i >> 1) & 1)) =
                         make_float4(fmaf(o[t][i][c] * un, f, sv[c]), fmaf((o[t][i + 1][c] - less * o[t][i][c]) * un, f * 0.0625f, sv[c]),
                                     fmaf(o[t][i][c + 2] * un, f, sv[c]), fmaf((o[t][i + 1][c + 2] - less * o[t][i][c + 2]) * un, f * 0.0625f, sv[c]));

@@ -1,0 +1,104 @@
+"""The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight."""
+import numpy as np
+import pytest
+import torch
+
+import kv_reference as ref
+import paper_2211_04515_b200 as qp
+from test_kv_cache import BF16, F32, ctx, halves, ints, lib, make  # noqa: F401  (fixtures among them)
+
+
+def bound_of(q, k, v, seen, scale, dtype, in_halves):
+    """One query over the rows that it sees, fp64: (out, bound of |error|, bound of |difference| between the results of two calls whose
+    rows of K are the same).  Nothing in the bounds comes from a row of V without weight: every term is weighted by p.  k, v as
+    kv_reference.sequence gives them."""
+    kv, klo, ks, _ = (x[seen] for x in k)
+    vv, vlo, vs, vc = (x[seen] for x in v)
+    s = kv @ q * scale
+    p = np.exp(s - s.max())
+    l = p.sum()
+    out = p @ vv / l
+    n = len(s)
+    # a score's error as in kv_reference.attention_row, but each row's own; it changes its weight by at most twice that share
+    ds = 2.0 ** -17 * abs(scale) * np.abs(q).sum() * (np.abs(klo) + 15 * ks)
+    held = np.abs(vlo) + 15 * vs                                 # magnitudes that the sums are made of
+    # weights in 11 (bf16) or 22 bits; below fp16's normal numbers to 2^-25, where the largest p * vs is 2^7 or more
+    eps = 2.0 ** -11 if dtype == BF16 else 2.0 ** -21
+    weights = eps * (p * vs) @ vc / l + n * 15 * 2.0 ** -32 * (p * vs).max() / l
+    v_off = 0.0
+    if in_halves:
+        # K and V in fp16: of the value 2^-11, of the middle of the row 2^-11, of the scale 2^-11 times at most 8; K by a tile's power of
+        # two (2^-34 of the tile's largest, here of the largest seen)
+        def rounding(x, lo, scale):
+            return 2.0 ** -11 * (np.abs(x) + (np.abs(lo + 8 * scale) + 8 * scale)[:, None])
+        ds = ds + abs(scale) * ((rounding(kv, klo, ks) + 2.0 ** -34 * np.abs(kv).max()) @ np.abs(q))
+        # Weights: 2^-11, and 2^-25 below the normal numbers.  A row's own largest value is at 2^2 or above in its tile (up to 2^11), and the
+        # largest p * (row's largest value) stands at 2^(5 - 8) * 2^2 or above.  So 2^-25 * 2^11 is 2^-13 of that, and a
+        # subnormal value's 2^-25, twice, 2^-26 of its row's largest.
+        most = np.abs(vv).max(1)
+        small = p @ np.repeat((2.0 ** -26 * most)[:, None], vv.shape[1], 1) / l
+        weights = 2.0 ** -11 * p @ np.abs(vv) / l + n * 2.0 ** -13 * (p * most).max() / l + small
+        v_off = p @ rounding(vv, vlo, vs) / l
+    # exp2 2^-21 and its argument 2^-20, fp32 sums n / 8 steps; the matrix unit drops leading zeros of a subnormal code (bf16): 2^-16
+    each = 2.0 ** -19 + (n / 8 + 16) * 2.0 ** -24 + (2.0 ** -16 if dtype == BF16 else 0)
+
+    def moved(by):                                               # weights off by these shares
+        return p @ (by * held) / l + (p @ by / l) * (p @ held / l)
+    same = moved(np.full(n, each)) + weights
+    err = same + moved(2 * ds) + v_off
+    half = torch.finfo(dtype).eps / 2
+    return out, err + half * (np.abs(out) + err), 2 * (same + half * (np.abs(out) + err))
+
+
+OUTLIERS = [
+    # dim, dtype, group, new, window
+    (128, BF16, 4, 1, 0), (128, F32, 4, 1, 0), (64, F32, 1, 1, 0), (256, BF16, 2, 1, 0), (256, F32, 3, 4, 0),
+    (128, BF16, 8, 1, 700), (64, F32, 2, 3, 700), (128, BF16, 4, 9, 0), (64, BF16, 16, 2, 300), (128, F32, 4, 9, 500),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("octaves", [12, 24, 60])
+@pytest.mark.parametrize("case", OUTLIERS, ids=str)
+def test_values_without_weight(ctx, case, octaves):
+    """Rows of V that are 2^octaves times as large as the others but are masked for a query, lie in front of its window or have no
+    weight: they leave no trace in its result."""
+    dim, dtype, group, new, window = case
+    rng = np.random.default_rng(dim + new + octaves)
+    n, page = 1999, 32
+    cache = make(rng, [n], 1, dim, page)
+    base = rng.standard_normal(dim)
+    base *= dim ** 0.5 / np.linalg.norm(base)
+    k = rng.standard_normal((n, 1, dim)) * 0.7
+    v = rng.standard_normal((n, 1, dim)) * rng.uniform(0.3, 1.5, (n, 1, 1))
+    big = [5, 700, n - new - 1]                                     # without weight
+    k[big] = -8 * base                                              # 8 * sqrt(dim) below, in nats
+    later = [n - 1] + ([n - new // 2] if new > 2 else [])           # masked for the rows in front of them
+    k[later] = -8 * base
+    before = [n - new - window - 1, n - new - window - 5] if window else []    # seen by nobody, in slices that are read
+    v[40] = 0                                                       # a row of zeros, and one much smaller than the others
+    v[41] *= 2.0 ** -30
+    k = torch.from_numpy(k.astype(np.float32)).cuda()
+    q = torch.from_numpy((base + 1.2 * rng.standard_normal((new, group, dim))).astype(np.float32)).cuda().to(dtype)
+    batch = qp.KVBatch(ints([n - new]), start=ints([0, new]), tokens=new, max_new=new)
+    plan = ctx.qp_kv_attention_plan(cache, group, window)
+    got, rows = [], []
+    for times in (1.0, 2.0 ** octaves):
+        v[big + later + before] *= times
+        ctx.qp_kv_append(cache, qp.KVBatch(ints([0]), start=ints([0, n]), tokens=n, max_new=n), k, torch.from_numpy(v.astype(np.float32)).cuda())
+        got.append(ctx.qp_kv_attention(cache, batch, q, plan, out=torch.empty_like(q)).double().cpu().numpy())
+        rows.append(ref.sequence(cache.pool[0].cpu().numpy(), cache.table[0].cpu().numpy(), 0, n, page, dim))
+    assert ctx.qp_get_status() == 0
+    qn = q.double().cpu().numpy()
+    u = np.arange(n)
+    for i in range(new):
+        t = n - new + i
+        seen = (u <= t) & ((u > t - window) if window else True)
+        for g in range(group):
+            wants = [bound_of(qn[i, g], *r, seen, dim ** -0.5, dtype, halves(dtype, dim, new * group)) for r in rows]
+            apart = np.abs(got[1][i, g] - got[0][i, g])
+            limit = np.abs(wants[1][0] - wants[0][0]) + np.maximum(wants[0][2], wants[1][2])
+            assert (apart <= limit).all(), (i, g, float((apart / limit).max()), float(apart.max()), float(np.abs(wants[0][0]).max()))
+            for have, (want, bound, _) in zip(got, wants):
+                off = np.abs(have[i, g] - want)
+                assert (off <= bound).all(), (i, g, float((off / bound).max()), float(off.max()), float(np.abs(want).max()))
