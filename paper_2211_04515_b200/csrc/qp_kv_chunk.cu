@@ -18,9 +18,11 @@
 // The result, scale and the value of code 8 are each rounded to 11 bits, an eighth of what bf16 would lose.  (About code 0 instead: lo is
 // several times the middle of a row, and its rounding moves a whole row of scores; the result was 1.6 times as far off.)  fp16's range: each tile of K and of V is scaled by a power of two that takes its largest
 // value to [2^10, 2^11); queries are scaled by row.  K's power goes into the factor of the scores, V's into the exponent of
-// the weights (both are one number a tile).  Elements lie in the order 0 4 1 5 2 6 3 7 of each eight, in the operands and in O.
+// the weights (both are one number a tile).  A tile whose rows of V are of very different sizes has a power for each of them, which
+// goes into each weight's exponent.  Elements lie in the order 0 4 1 5 2 6 3 7 of each eight, in the operands and in O.
 //
-//   - Softmax reference raised only when a score passes it by 8 (log2): then O is read from tensor memory, scaled and put back.
+//   - Softmax reference raised only when a score passes it by 8 (log2).  O has another, of the scores plus V's powers: raised likewise, and then O
+//     is read from tensor memory, scaled and put back.
 //   - The work, in key tiles, is cut into equal runs for the SMs; an item that a cut falls into leaves partial results
 //     and the last block to finish adds them (as for few queries).
 //   - Registers: 128 a thread at launch; the softmax warps go to 160 (a row's 64 scores stay in registers), the issuing warp's group
@@ -45,6 +47,10 @@ constexpr int MIN_RUN = 4;                       // key tiles that are worth a b
 constexpr int SEGS = 32;                         // parts of items that are listed at a time
 constexpr float M_NONE = -3.0e38f, M_SLACK = 8.f;
 constexpr int P_SHIFT = 5;                       // weights are 2^5 higher: up to 2^13 in fp16
+// A tile whose rows of V have largest values further apart than this (log2) has a power of two for each row.  Always so: 1330 us for 2048 tokens
+// over 9001 and 16384, never (no such tile): 956.  One power for rows 2^7 apart costs weights that stand at 2^8 or above seven of the 32 powers
+// of two that fp16 has below that.
+constexpr int V_SPREAD = 7;
 
 template <int D> struct Cfg {
     static constexpr int OPERAND = TILE * D * 2;                 // bytes of Q, K, V tiles
@@ -199,7 +205,10 @@ struct Shared {
     int2 about[2];
     uint4 valid[2];
     float2 quant[2][2][TILE];                    // K's and V's quantizers of a tile
-    float amax[2][2][4];
+    alignas(16) float row_power[2][TILE];        // where V's rows are scaled one by one (spread), a row's power of two less the tile's
+    int spread[2];
+    unsigned amax[2][2][4];                      // per 32 keys the largest value of K and of V (bits of a float),
+    int vmin[2][4];                              // and the smallest power of a row of V
     int last[2];
     Seg segs[SEGS];
 };
@@ -323,6 +332,9 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
     for (int i = 0; i < sh.n_segs; ++i) {
         const Seg& s = sh.segs[i];
         const int held = s.pos + s.n, units = s.u1 - s.u0;
+        // keys that some row of the item sees: the others must not count where a power of two is chosen for a tile
+        const int row0 = s.tile * ROWS, row1 = min(row0 + ROWS, s.n * a.group);
+        const int seen0 = a.window > 0 ? s.pos + row0 / a.group - a.window + 1 : 0, seen1 = s.pos + (row1 - 1) / a.group + 1;
         // what a tile needs from memory, in registers: asked for one tile ahead, its places two
         struct Raw { uint4 k[L], v[L]; float4 quant; unsigned there; } now, next;
         int64_t place = -1;
@@ -345,7 +357,8 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
             }
             const int64_t mine = __shfl_sync(0xFFFFFFFFu, place, p / QP_KV_SLICE);
             x.quant = make_float4(0.f, 0.f, 0.f, 0.f);
-            const bool there = mine >= 0 && (s.s0 + 8 * u) * QP_KV_SLICE + p < held;
+            const int key = (s.s0 + 8 * u) * QP_KV_SLICE + p;
+            const bool there = mine >= 0 && key >= seen0 && key < seen1;
             if (there) {
                 const float2 kq = qp_kv_ld(reinterpret_cast<const float2*>(a.pool + mine + S::KQ + p % QP_KV_SLICE * 8));
                 const float2 vq = qp_kv_ld(reinterpret_cast<const float2*>(a.pool + mine + S::VQ + p % QP_KV_SLICE * 8));
@@ -356,25 +369,30 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
         auto convert = [&](Raw& x) {
             const int st = g & 1;
             const float4 quant = x.quant;
-            // powers of two for the tile
-            float ka = fmaxf(fabsf(quant.x), fabsf(fmaf(15.f, quant.y, quant.x))), va = fmaxf(fabsf(quant.z), fabsf(fmaf(15.f, quant.w, quant.z)));
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                ka = fmaxf(ka, __shfl_xor_sync(0xFFFFFFFFu, ka, o));
-                va = fmaxf(va, __shfl_xor_sync(0xFFFFFFFFu, va, o));
-            }
-            if (lane == 0) { sh.amax[st][0][p >> 5] = ka; sh.amax[st][1][p >> 5] = va; }
+            // powers of two for the tile, which take its largest value to [2^10, 2^11) (not below -100: nothing to gain)
+            const unsigned mine = __float_as_uint(fmaxf(fabsf(quant.z), fabsf(fmaf(15.f, quant.w, quant.z))));
+            const unsigned ka = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(fabsf(quant.x), fabsf(fmaf(15.f, quant.y, quant.x)))));
+            const unsigned va = __reduce_max_sync(0xFFFFFFFFu, mine);
+            const int own = max((int)(mine >> 23) - 137, -100), vmin = __reduce_min_sync(0xFFFFFFFFu, x.there >> lane & 1u ? own : 1000);
+            if (lane == 0) { sh.amax[st][0][p >> 5] = ka; sh.amax[st][1][p >> 5] = va; sh.vmin[st][p >> 5] = vmin; }
             sh.quant[st][0][p] = make_float2(quant.x, quant.y);
             sh.quant[st][1][p] = make_float2(quant.z, quant.w);
             group_sync<1>();
+            unsigned kb = 0, vb = 0;
+            int least = 1000;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) { ka = fmaxf(ka, sh.amax[st][0][w]); va = fmaxf(va, sh.amax[st][1][w]); }
-            int ke = (int)(__float_as_uint(ka) >> 23) - 127 - 10, ve = (int)(__float_as_uint(va) >> 23) - 127 - 10;
-            ke = ke < -100 ? -100 : ke;                          // (all but zero: nothing to gain)
-            ve = ve < -100 ? -100 : ve;
-            const float kf = pow2(-ke), vf = pow2(-ve);
+            for (int w = 0; w < 4; ++w) { kb = max(kb, sh.amax[st][0][w]); vb = max(vb, sh.amax[st][1][w]); least = min(least, sh.vmin[st][w]); }
+            const int ke = max((int)(kb >> 23) - 137, -100), ve = max((int)(vb >> 23) - 137, -100);
+            const bool spread = ve - least > V_SPREAD;           // (the same in all threads)
+            const float kf = pow2(-ke), vf = spread ? 1.f : pow2(-ve);
             if (g >= 2) wait(sh, &sh.kv_empty[st], ((g >> 1) + 1) & 1, a.wait_cycles);
             __syncwarp();
+            if (spread) {
+                const float f = pow2(-own);
+                sh.quant[st][1][p] = make_float2(quant.z * f, quant.w * f);
+                sh.row_power[st][p] = (float)(own - ve);
+                group_sync<1>();
+            }
             char* to = stages + st * (2 * C::OPERAND);
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {                        // K, then V
@@ -402,7 +420,7 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
 #pragma unroll
                 for (int l = 0; l < L; ++l) x.k[l] = x.v[l];
             }
-            if (p == 0) sh.about[st] = make_int2(__float_as_int(pow2(ke)), ve);
+            if (p == 0) { sh.about[st] = make_int2(__float_as_int(pow2(ke)), ve); sh.spread[st] = spread; }
             if (lane == 0) (&sh.valid[st].x)[p >> 5] = x.there;
             fence_operands();
             arrive(&sh.kv_full[st]);
@@ -574,8 +592,9 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         const int hi = (int)min((int64_t)s.pos + (mine ? r : all - 1) / a.group, (int64_t)0x7FFFFFFF);
         const int all_hi = (int)min((int64_t)s.pos + row0 / a.group, (int64_t)0x7FFFFFFE) + 1;
         const int all_lo = a.window > 0 ? (int)min((int64_t)s.pos + last_row / a.group - a.window, (int64_t)0x7FFFFFFE) + 1 : 0;
-        float m = M_NONE, l = 0.f;
-        int E = -1000;                                           // O holds sums of p * v * 2^(P_SHIFT - E)
+        // p = 2^(s - m) in l; O holds sums of 2^(s + P_SHIFT - X) * v.  X follows the largest s + (power of two of the tile's V), of keys that the
+        // row sees: weights of 2^13 at most in fp16, and none lost that counts, whatever the other rows and tiles hold.
+        float m = M_NONE, X = M_NONE, l = 0.f;
         const int first_key = s.s0 * QP_KV_SLICE, u0 = s.u0, u1 = s.u1;
         for (int u = u0; u < u1; ++u, ++g) {
             const int st = g & 1;
@@ -583,7 +602,9 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
             const int2 about = sh.about[st];
             const uint4 v4 = sh.valid[st];
             const float f = fmaxf(kf * __int_as_float(about.x), 1e-37f);         // (positive, so that -inf stays)
-            const int ve = about.y, key0 = first_key + u * TILE;
+            const float ve = (float)about.y;
+            const bool spread = sh.spread[st] != 0;
+            const int key0 = first_key + u * TILE;
             const bool whole = (v4.x & v4.y & v4.z & v4.w) == 0xFFFFFFFFu && key0 >= all_lo && key0 + TILE <= all_hi;
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
@@ -612,15 +633,22 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
 #pragma unroll
                     for (int e = 0; e < 4; ++e) top4[e] = c + 4 + e < HALF ? qp_max3(top4[e], x[c + e], x[c + 4 + e]) : fmaxf(top4[e], x[c + e]);
                 const float top = fmaxf(qp_max3(top4[0], top4[1], top4[2]), top4[3]) * f;
-                if (__any_sync(0xFFFFFFFFu, top > m + M_SLACK || ve > E)) {     // rare: a new reference
-                    const float next = fmaxf(m, top);
-                    float back = ex2(m - next);
-                    m = next;
-                    l *= back;
-                    if (ve > E) {
-                        back *= E < -999 ? 0.f : pow2(E - ve);
-                        E = ve;
+                const float* power = sh.row_power[st] + h * HALF;
+                float most = top;
+                if (spread) {                                    // uncommon: rows of V scaled one by one
+                    most = -inf;
+#pragma unroll
+                    for (int c = 0; c < HALF; c += 4) {
+                        const float4 r = *reinterpret_cast<const float4*>(power + c);
+                        most = fmaxf(qp_max3(most, fmaf(x[c], f, r.x), fmaf(x[c + 1], f, r.y)), fmaxf(fmaf(x[c + 2], f, r.z), fmaf(x[c + 3], f, r.w)));
                     }
+                }
+                most += ve;
+                if (__any_sync(0xFFFFFFFFu, top > m + M_SLACK || most > X + M_SLACK)) {     // rare: new references
+                    const float next = fmaxf(m, top), to = fmaxf(X, most), back = ex2(X - to);
+                    l *= ex2(m - next);
+                    m = next;
+                    X = to;
                     if (u > u0 || h > 0) {
                         wait(sh, &sh.pv_done[t][h ^ 1], (h ? g : g - 1) & 1, a.wait_cycles);      // of the half before
                         __syncwarp();
@@ -637,10 +665,25 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
                         wait_st();
                     }
                 }
-                // (where V is so small against what O holds that its weights leave fp16, they must not leave fp32, for the sum's sake)
-                const int up2 = ve - E < -90 ? -90 : ve - E;
-                const float sub = (float)(P_SHIFT + up2) - m;
-                const qp_f2 f2 = qp_pack2(f, f), sub2 = qp_pack2(sub, sub);
+                float sub = (float)P_SHIFT + ve - X, fw = f, lift = 0.f;
+                if (!spread) {
+                    // (where V is so small against what O holds that its weights leave fp16, they must not leave fp32, for the sum's sake)
+                    sub = fmaxf(sub, (float)(P_SHIFT - 90) - m);
+                    lift = ex2(-m - sub);
+                } else {
+                    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+                    for (int c = 0; c < HALF; c += 4) {
+                        const float4 r = *reinterpret_cast<const float4*>(power + c);
+                        s0 += ex2(fmaf(x[c], f, -m)) + ex2(fmaf(x[c + 1], f, -m));
+                        s1 += ex2(fmaf(x[c + 2], f, -m)) + ex2(fmaf(x[c + 3], f, -m));
+                        x[c] = fmaf(x[c], f, r.x); x[c + 1] = fmaf(x[c + 1], f, r.y);
+                        x[c + 2] = fmaf(x[c + 2], f, r.z); x[c + 3] = fmaf(x[c + 3], f, r.w);
+                    }
+                    l += s0 + s1;
+                    fw = 1.f;
+                }
+                const qp_f2 f2 = qp_pack2(fw, fw), sub2 = qp_pack2(sub, sub);
                 qp_f2 sum = qp_pack2(0.f, 0.f), sum1 = sum;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
@@ -659,7 +702,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
                 }
                 float s0, s1;
                 qp_unpack2(qp_add2(sum, sum1), s0, s1);
-                l = fmaf(s0 + s1, pow2(-up2 - P_SHIFT), l);
+                l = fmaf(s0 + s1, lift, l);
                 wait_st();
                 fence_before();
                 arrive(&sh.p_full[t][h]);
@@ -673,7 +716,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         float* part = a.part + ((int64_t)s.at * 2 + t) * C::PART;
         const int token = s.row0 + r / a.group, head = s.head * a.group + r % a.group;      // (of a row that is there)
         unsigned short* to = static_cast<unsigned short*>(a.out) + (int64_t)token * a.ot + (int64_t)head * a.oh;
-        const float un = pow2(E - P_SHIFT), over = s.split ? 1.f : l == 0.f ? 0.f : 1.f / l;
+        const float un = ex2(X - m - (float)P_SHIFT), over = s.split ? 1.f : l == 0.f ? 0.f : 1.f / l;
 #pragma unroll 1
         for (int c = 0; c < D / 32; ++c) {
             float y[32];

@@ -1,4 +1,4 @@
-"""The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight."""
+"""The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or X
 import numpy as np
 import pytest
 import torch
@@ -32,12 +32,12 @@ def bound_of(q, k, v, seen, scale, dtype, in_halves):
         def rounding(x, lo, scale):
             return 2.0 ** -11 * (np.abs(x) + (np.abs(lo + 8 * scale) + 8 * scale)[:, None])
         ds = ds + abs(scale) * ((rounding(kv, klo, ks) + 2.0 ** -34 * np.abs(kv).max()) @ np.abs(q))
-        # Weights: 2^-11, and 2^-25 below the normal numbers.  A row's own largest value is at 2^2 or above in its tile (up to 2^11), and the
-        # largest p * (row's largest value) stands at 2^(5 - 8) * 2^2 or above.  So 2^-25 * 2^11 is 2^-13 of that, and a
-        # subnormal value's 2^-25, twice, 2^-26 of its row's largest.
+        # Weights: 2^-11, and 2^-25 below the normal numbers.  A row's own largest value stands at 2^3 or above in its tile (below 2^11), so
+        # that a subnormal value's 2^-25, twice, is at most 2^-26 of it.  The weight that O's reference was taken from is 2^5 or more, so
+        # the largest p * (row's largest value) stands at 2^8 or above, and 2^-25 * 2^11 is 2^-22 of that.
         most = np.abs(vv).max(1)
         small = p @ np.repeat((2.0 ** -26 * most)[:, None], vv.shape[1], 1) / l
-        weights = 2.0 ** -11 * p @ np.abs(vv) / l + n * 2.0 ** -13 * (p * most).max() / l + small
+        weights = 2.0 ** -11 * p @ np.abs(vv) / l + n * 2.0 ** -22 * (p * most).max() / l + small
         v_off = p @ rounding(vv, vlo, vs) / l
     # exp2 2^-21 and its argument 2^-20, fp32 sums n / 8 steps; the matrix unit drops leading zeros of a subnormal code (bf16): 2^-16
     each = 2.0 ** -19 + (n / 8 + 16) * 2.0 ** -24 + (2.0 ** -16 if dtype == BF16 else 0)
@@ -54,6 +54,7 @@ OUTLIERS = [
     # dim, dtype, group, new, window
     (128, BF16, 4, 1, 0), (128, F32, 4, 1, 0), (64, F32, 1, 1, 0), (256, BF16, 2, 1, 0), (256, F32, 3, 4, 0),
     (128, BF16, 8, 1, 700), (64, F32, 2, 3, 700), (128, BF16, 4, 9, 0), (64, BF16, 16, 2, 300), (128, F32, 4, 9, 500),
+    (128, BF16, 4, 80, 0), (64, BF16, 2, 100, 0), (128, BF16, 3, 150, 650), (64, BF16, 4, 300, 0),
 ]
 
 
@@ -102,3 +103,34 @@ def test_values_without_weight(ctx, case, octaves):
             for have, (want, bound, _) in zip(got, wants):
                 off = np.abs(have[i, g] - want)
                 assert (off <= bound).all(), (i, g, float((off / bound).max()), float(off.max()), float(np.abs(want).max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", OUTLIERS, ids=str)
+def test_values_of_many_sizes(ctx, case):
+    """Every row of V has a size of its own, 24 octaves between them, and the scores go up along the sequence or down."""
+    dim, dtype, group, new, window = case
+    rng = np.random.default_rng(dim + new)
+    n, page = 1200, 16
+    cache = make(rng, [n, n], 1, dim, page)
+    base = rng.standard_normal(dim)
+    base *= dim ** 0.5 / np.linalg.norm(base)
+    slope = np.concatenate((np.linspace(-1.5, 1.5, n), np.linspace(1, -1, n)))[:, None, None]
+    k = (rng.standard_normal((2 * n, 1, dim)) * 0.5 + slope * base).astype(np.float32)
+    v = (rng.standard_normal((2 * n, 1, dim)) * 2.0 ** rng.uniform(-12, 12, (2 * n, 1, 1))).astype(np.float32)
+    v[rng.integers(0, 2 * n, 200)] = 0
+    ctx.qp_kv_append(cache, qp.KVBatch(ints([0, 0]), start=ints([0, n, 2 * n]), tokens=2 * n, max_new=n), *(torch.from_numpy(x).cuda() for x in (k, v)))
+    q = torch.from_numpy((base + 0.8 * rng.standard_normal((2 * new, group, dim))).astype(np.float32)).cuda().to(dtype)
+    batch = qp.KVBatch(ints([n - new] * 2), start=ints([0, new, 2 * new]), tokens=2 * new, max_new=new)
+    out = ctx.qp_kv_attention(cache, batch, q, ctx.qp_kv_attention_plan(cache, group, window), out=torch.empty_like(q)).double().cpu().numpy()
+    assert ctx.qp_get_status() == 0
+    u = np.arange(n)
+    for b in range(2):
+        rows = ref.sequence(cache.pool[0].cpu().numpy(), cache.table[b].cpu().numpy(), 0, n, page, dim)
+        for i in range(new):
+            t = n - new + i
+            seen = (u <= t) & ((u > t - window) if window else True)
+            for g in range(group):
+                want, bound, _ = bound_of(q[b * new + i, g].double().cpu().numpy(), *rows, seen, dim ** -0.5, dtype, halves(dtype, dim, new * group))
+                off = np.abs(out[b * new + i, g] - want)
+                assert (off <= bound).all(), (b, i, g, float((off / bound).max()), float(off.max()), float(np.abs(want).max()))
