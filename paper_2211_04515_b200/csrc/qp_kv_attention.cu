@@ -189,6 +189,9 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
         q.n = a.max_new;
     }
     derive<ROWS>(a, q);
+    // tokens behind the last page that the table has room for: counted as masked (the same for sequences that qp_kv_chunk.cu takes)
+    const int most = a.pages.max_pages * a.pages.page_size;      // (below 2^31 - 4096)
+    if (blockIdx.x == 0 && q.n > 0 && q.pos >= 0 && q.pos <= 0x7FFFFFFF - q.n && q.pos + q.n > most) atomicOr(a.status, QP_DEV_KV_RANGE);
     return q;
 }
 

@@ -1,11 +1,12 @@
-"""The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or X
+"""The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
+table."""
 import numpy as np
 import pytest
 import torch
 
 import kv_reference as ref
 import paper_2211_04515_b200 as qp
-from test_kv_cache import BF16, F32, ctx, halves, ints, lib, make  # noqa: F401  (fixtures among them)
+from test_kv_cache import BF16, F32, ctx, fill, halves, ints, lib, make  # noqa: F401  (fixtures among them)
 
 
 def bound_of(q, k, v, seen, scale, dtype, in_halves):
@@ -134,3 +135,34 @@ def test_values_of_many_sizes(ctx, case):
                 want, bound, _ = bound_of(q[b * new + i, g].double().cpu().numpy(), *rows, seen, dim ** -0.5, dtype, halves(dtype, dim, new * group))
                 off = np.abs(out[b * new + i, g] - want)
                 assert (off <= bound).all(), (b, i, g, float((off / bound).max()), float(off.max()), float(np.abs(want).max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,group,new,window", [(BF16, 4, 1, 0), (F32, 2, 1, 20), (BF16, 4, 7, 0), (BF16, 8, 40, 0), (BF16, 4, 60, 50),
+                                                    (F32, 1, 30, 10)])
+@pytest.mark.parametrize("past", [1, 20, 300])
+def test_positions_past_the_table(ctx, dtype, group, new, window, past):
+    """Tokens behind the last page that the table has room for count as masked, and are reported."""
+    rng = np.random.default_rng(past)
+    dim, page, full = 128, 16, 416
+    cache = make(rng, [full], 1, dim, page, max_pages=full // page)
+    fill(ctx, rng, cache, [full])
+    end = full + past                                               # behind the last query's position
+    q = torch.from_numpy(rng.standard_normal((new, group, dim)).astype(np.float32)).cuda().to(dtype)
+    plan = ctx.qp_kv_attention_plan(cache, group, window)
+    lse = torch.empty(new, group, device="cuda")
+    for pos, status in ((full - new, 0), (end - new, qp.QP_DEV_KV_RANGE)):
+        batch = qp.KVBatch(ints([pos]), start=ints([0, new]), tokens=new, max_new=new)
+        out = ctx.qp_kv_attention(cache, batch, q, plan, lse=lse)
+        assert ctx.qp_get_status() == status
+        k, v = ref.sequence(cache.pool[0].cpu().numpy(), cache.table[0].cpu().numpy(), 0, full, page, dim)
+        u = np.arange(full)
+        for i in range(new):
+            t = pos + i
+            seen = (u <= t) & ((u > t - window) if window else True)
+            for g in range(group):
+                if not seen.any():
+                    assert (out[i, g] == 0).all() and lse[i, g] == -np.inf
+                    continue
+                want, bound, _ = bound_of(q[i, g].double().cpu().numpy(), k, v, seen, dim ** -0.5, dtype, halves(dtype, dim, new * group))
+                assert (np.abs(out[i, g].double().cpu().numpy() - want) <= bound).all()
