@@ -58,6 +58,8 @@ struct qp_kv_rows {
 };
 static inline qp_kv_rows qp_kv_rows_of(const qp_kv_batch_t* b) { return {b->d_slots, b->d_start, b->d_pos, b->batch, b->tokens}; }
 
+// row that sequence b begins with, the end of the one before it; within the rows that there are, so that no row at or behind
+// `tokens` is anybody's
 __device__ __forceinline__ int qp_kv_start(const qp_kv_rows& r, int b)
 {
     const int s = r.start ? qp_kv_ld(r.start + b) : b;

@@ -182,8 +182,7 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
     q.pos = qp_kv_ld(a.rows.pos + b);
     q.slot = qp_kv_slot(a.rows, b);
     q.row0 = qp_kv_start(a.rows, b);
-    const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
-    q.n = row1 - q.row0;
+    q.n = qp_kv_start(a.rows, b + 1) - q.row0;
     if (q.n > a.max_new) {                                       // (every block comes here for every sequence; one says so)
         if (blockIdx.x == 0) atomicOr(a.status, QP_DEV_KV_RANGE);
         q.n = a.max_new;

@@ -221,8 +221,7 @@ __device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
     q.pos = qp_kv_ld(a.rows.pos + b);
     q.slot = qp_kv_slot(a.rows, b);
     q.row0 = qp_kv_start(a.rows, b);
-    const int row1 = a.rows.start ? qp_kv_start(a.rows, b + 1) : (b < a.rows.tokens ? b + 1 : b);
-    q.n = row1 - q.row0;
+    q.n = qp_kv_start(a.rows, b + 1) - q.row0;
     if (q.n > a.max_new) q.n = a.max_new;
     const int64_t rows = (int64_t)q.n * a.group;
     q.tiles = q.n <= 0 || q.pos < 0 || q.pos > 0x7FFFFFFF - q.n || rows < a.many ? 0 : (int)((rows + ROWS - 1) / ROWS);

@@ -1,12 +1,12 @@
 """The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
-table."""
+table, more sequences than rows."""
 import numpy as np
 import pytest
 import torch
 
 import kv_reference as ref
 import paper_2211_04515_b200 as qp
-from test_kv_cache import BF16, F32, ctx, fill, halves, ints, lib, make  # noqa: F401  (fixtures among them)
+from test_kv_cache import BF16, F32, check_attention, ctx, fill, halves, ints, lib, make  # noqa: F401  (fixtures among them)
 
 
 def bound_of(q, k, v, seen, scale, dtype, in_halves):
@@ -166,3 +166,30 @@ def test_positions_past_the_table(ctx, dtype, group, new, window, past):
                     continue
                 want, bound, _ = bound_of(q[i, g].double().cpu().numpy(), k, v, seen, dim ** -0.5, dtype, halves(dtype, dim, new * group))
                 assert (np.abs(out[i, g].double().cpu().numpy() - want) <= bound).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,group", [(BF16, 4), (F32, 2), (BF16, 160), (BF16, 16)])
+def test_batches_of_more_sequences_than_rows(ctx, dtype, group):
+    """Without start sequence b has row b: those at and behind `tokens` have none, and no row behind is read or written."""
+    rng = np.random.default_rng(26)
+    dim, lens, tokens = 64, [60, 100, 40, 70, 90, 33, 21], 3
+    cache = make(rng, lens, 1, dim, 16)
+    k, v = fill(ctx, rng, cache, lens)
+    q = torch.from_numpy(rng.standard_normal((8, group, dim)).astype(np.float32)).cuda().to(dtype)
+    pos = [n - 1 for n in lens]
+    for slots in (None, ints(range(7))):
+        batch = qp.KVBatch(ints(pos), slots=slots, tokens=tokens)
+        plan = ctx.qp_kv_attention_plan(cache, group)
+        out, lse = torch.full_like(q, 5.0), torch.full((8, group), 5.0, device="cuda")
+        ctx.qp_kv_attention(cache, batch, q, plan, out=out, lse=lse)
+        assert (out[tokens:] == 5).all() and (lse[tokens:] == 5).all() and ctx.qp_get_status() == 0
+        check_attention(ctx, cache, lens, range(3), pos[:3], np.arange(4), q, 0, out, lse, dim ** -0.5)
+        ko, vo = torch.full((8, 1, dim), 5.0, device="cuda"), torch.full((8, 1, dim), 5.0, device="cuda")
+        ctx.qp_kv_gather(cache, batch, ko, vo)
+        assert (ko[tokens:] == 5).all() and (vo[tokens:] == 5).all() and (ko[:tokens] != 5).any()
+        before = cache.pool.clone()
+        ctx.qp_kv_append(cache, batch, ko, vo)
+        for s in range(tokens, 7):
+            ids = cache.table[s, :-(-lens[s] // 16)].long()
+            assert torch.equal(cache.pool[0, ids], before[0, ids])
