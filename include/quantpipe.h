@@ -654,13 +654,16 @@ int32_t qp_kv_gather(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batc
  * see, or gives next to no weight, have no part in that, however large they are.  A wait inside that kernel which does not end within the limit of
  * qp_set_wait_limit_for_testing raises QP_DEV_STREAM_TIMEOUT, as elsewhere.
  * The plan holds what stays from call to call; its workspace belongs to one stream at a time and is zeroed once,
- * before its first use (each call leaves its counters at zero). */
+ * before its first use (each call leaves its counters at zero).
+ * Rows of d_out that no sequence writes (behind the last, of sequences that take no part, beyond max_new) stay as they were; with
+ * QP_KV_ZERO_REST those among the first `tokens` become 0. */
+#define QP_KV_ZERO_REST 1
 typedef struct {
     void* d_work;
     uint64_t work_bytes;     /* at least qp_kv_attention_work_bytes */
     int32_t q_heads, window; /* window 0: none */
     float scale;
-    int32_t reserved;
+    int32_t flags;           /* 0 or QP_KV_ZERO_REST */
 } qp_kv_attention_t;         /* 32 bytes */
 uint64_t qp_kv_attention_work_bytes(qp_ctx* ctx, const qp_kv_cache_t* h_cache);
 int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batch_t* h_batch, const qp_kv_attention_t* h_plan,

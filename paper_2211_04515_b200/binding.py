@@ -30,6 +30,7 @@ QP_B_MAD, QP_B_MEAN_ABS = 0, 1
 QP_DEV_BITS_MISMATCH, QP_DEV_DEGENERATE, QP_DEV_NONFINITE, QP_DEV_STREAM_TIMEOUT, QP_DEV_HIST_MISSING = 1, 2, 4, 8, 16
 QP_DEV_INDEX_RANGE = 32
 QP_DEV_KV_RANGE, QP_DEV_KV_EXHAUSTED = 64, 128
+QP_KV_ZERO_REST = 1
 QP_DEFAULT_STEPS, QP_DEFAULT_HIST_BINS = 100, 100
 QP_SEARCH_AUTO, QP_SEARCH_CANDIDATES, QP_SEARCH_INTERVALS, QP_SEARCH_INTERVALS_PLAIN = 0, 1, 2, 3
 QP_SENDER_AUTO, QP_SENDER_CHAIN, QP_SENDER_FUSED = 0, 1, 2
@@ -94,7 +95,7 @@ class KVBatchDesc(C.Structure):
 
 class KVAttentionDesc(C.Structure):
     _fields_ = [("d_work", C.c_void_p), ("work_bytes", C.c_uint64), ("q_heads", C.c_int32), ("window", C.c_int32),
-                ("scale", C.c_float), ("reserved", C.c_int32)]
+                ("scale", C.c_float), ("flags", C.c_int32)]
 
 
 QP_CTRL_FIT, QP_CTRL_EQ2 = 0, 1
@@ -455,6 +456,9 @@ class KVAttention:
         self._index = work.get_device()
         self._desc = KVAttentionDesc(work.data_ptr(), work.nbytes, q_heads, window, scale, 0)
         self._at = C.addressof(self._desc)
+        # of calls that make their output: rows that no sequence writes are zero
+        self._desc_new = KVAttentionDesc(work.data_ptr(), work.nbytes, q_heads, window, scale, QP_KV_ZERO_REST)
+        self._at_new = C.addressof(self._desc_new)
 
 
 class Context:
@@ -773,18 +777,23 @@ class Context:
 
     def qp_kv_attention(self, cache: KVCache, batch: KVBatch, q: torch.Tensor, plan: KVAttention, layer: int = 0,
                         out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
-        """Attention of q [tokens, q_heads, head_dim] over the cache; writes out (q's type) and, if given, lse [tokens, q_heads]."""
+        """Attention of q [tokens, q_heads, head_dim] over the cache; writes out (q's type) and, if given, lse [tokens, q_heads].  Rows that no
+        sequence of the batch has are left as they were in out, and zero in a new tensor (out None)."""
         self._kv_here(cache, batch, plan)
         code, qt, qh = self._kv_rows(q, batch.tokens, plan.q_heads, cache.head_dim, "q")
+        at = plan._at
         if out is None:
             out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            at = plan._at_new
+            if out.shape[0] > batch.tokens:
+                out[batch.tokens:].zero_()
         out_code, ot, oh = self._kv_rows(out, batch.tokens, plan.q_heads, cache.head_dim, "out")
         if out_code != code:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "out must have q's type")
         if lse is not None and not (lse.dtype == torch.float32 and lse.get_device() == self._index and lse.is_contiguous()
                                     and lse.numel() >= batch.tokens * plan.q_heads):
             raise QuantPipeError(QP_ERR_INVALID_ARG, "lse must be a contiguous float32 tensor [tokens, q_heads]")
-        self._run("qp_kv_attention", cache._at, batch._at, plan._at, layer, q, code, qt, qh, out, ot, oh, lse)
+        self._run("qp_kv_attention", cache._at, batch._at, at, layer, q, code, qt, qh, out, ot, oh, lse)
         return out
 
     def qp_kv_fork(self, cache: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:

@@ -55,6 +55,9 @@ constexpr int HEAD = 6;
 // Units that are worth a block: 1 / 2 / 3 / 4 took 13.0 / 11.5 / 12.2 / 12.3 us for one sequence of 1021 tokens (16 parts to an item are
 // added in two levels, 8 in one); with more work than blocks there is no difference.
 constexpr int MIN_RUN = 2;
+// Blocks that are free of work at least, for the rows that no sequence writes where these become 0 (always, so that a call's bits do not depend
+// on it).
+constexpr unsigned REST_BLOCKS = 2;
 // Query rows of a sequence to a cached head from which on the tensor-memory kernel takes it.  This one against that, us, at 64 / 128 / 256
 // rows: 35 / 55 / 94 against 55 / 58 / 67 for 4 sequences of 4000 tokens and 8 heads; at 128 rows 94 against 71 for 16 of 4000
 // and 4 heads, 53 against 92 for one of 16000.
@@ -159,11 +162,12 @@ struct Seq {
     int64_t work;                                // units in all
 };
 
+__device__ __forceinline__ bool takes_part(const Seq& q) { return q.n > 0 && q.pos >= 0 && q.pos <= 0x7FFFFFFF - q.n; }
 // what follows from pos, n, row0 and slot
 template <int ROWS>
 __device__ __forceinline__ void derive(const qp_kv_attn_args& a, Seq& q)
 {
-    if (q.n <= 0 || q.pos < 0 || q.pos > 0x7FFFFFFF - q.n || (int64_t)q.n * a.group >= a.many) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return; }
+    if (!takes_part(q) || (int64_t)q.n * a.group >= a.many) { q.work = 0; q.units = q.tiles = 0; q.s0 = q.s1 = 0; return; }
     const unsigned most = (unsigned)a.pages.max_pages * (unsigned)a.pages.page_size;     // (below 2^31, as pos and n)
     const unsigned end0 = (unsigned)q.pos + (unsigned)q.n, end = end0 < most ? end0 : most;
     unsigned lo = a.window > 0 && q.pos >= a.window ? (unsigned)(q.pos - a.window + 1) : 0u;
@@ -175,22 +179,26 @@ __device__ __forceinline__ void derive(const qp_kv_attn_args& a, Seq& q)
     q.tiles = (int)(((unsigned)q.n * (unsigned)a.group + ROWS - 1) / ROWS);
     q.work = (int64_t)q.units * q.tiles * a.heads;
 }
+// rest: set if there are rows in front of the sequence, in it or behind it that nobody writes
 template <int ROWS>
-__device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b)
+__device__ __forceinline__ Seq seq_of(const qp_kv_attn_args& a, int b, bool* rest)
 {
     Seq q;
     q.pos = qp_kv_ld(a.rows.pos + b);
     q.slot = qp_kv_slot(a.rows, b);
     q.row0 = qp_kv_start(a.rows, b);
-    q.n = qp_kv_start(a.rows, b + 1) - q.row0;
+    const int row1 = qp_kv_start(a.rows, b + 1);
+    q.n = row1 - q.row0;
+    if (rest) *rest |= (b == 0 && q.row0 > 0) || (b == a.rows.batch - 1 && row1 < a.rows.tokens) || q.n < 0 || q.n > a.max_new;
     if (q.n > a.max_new) {                                       // (every block comes here for every sequence; one says so)
         if (blockIdx.x == 0) atomicOr(a.status, QP_DEV_KV_RANGE);
         q.n = a.max_new;
     }
     derive<ROWS>(a, q);
+    if (rest) *rest |= q.n > 0 && !takes_part(q);
     // tokens behind the last page that the table has room for: counted as masked (the same for sequences that qp_kv_chunk.cu takes)
     const int most = a.pages.max_pages * a.pages.page_size;      // (below 2^31 - 4096)
-    if (blockIdx.x == 0 && q.n > 0 && q.pos >= 0 && q.pos <= 0x7FFFFFFF - q.n && q.pos + q.n > most) atomicOr(a.status, QP_DEV_KV_RANGE);
+    if (blockIdx.x == 0 && takes_part(q) && q.pos + q.n > most) atomicOr(a.status, QP_DEV_KV_RANGE);
     return q;
 }
 
@@ -239,11 +247,11 @@ __device__ __forceinline__ void find_part(const qp_kv_attn_args& a, const Chunk&
     if (lane == 0) to = p;
 }
 template <int ROWS>
-__device__ __forceinline__ int64_t load_chunk(const qp_kv_attn_args& a, int b0, int64_t base, Chunk& sh)
+__device__ __forceinline__ int64_t load_chunk(const qp_kv_attn_args& a, int b0, int64_t base, Chunk& sh, bool* rest = nullptr)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, b = b0 + threadIdx.x;
     Seq q = {-1, 0, 0, 0, 0, 0, 0, 0, 0};
-    if (b < a.rows.batch) q = seq_of<ROWS>(a, b);
+    if (b < a.rows.batch) q = seq_of<ROWS>(a, b, rest);
     int64_t x = q.work;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -312,6 +320,27 @@ __device__ __forceinline__ void put_out(unsigned short* p, bool vec, const float
     else
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = h[i];
+}
+
+// Rows that no sequence writes become 0: the n blocks without a part of the work look at the whole batch for each row (uncommon: a padded
+// batch, sequences that take no part; in the other blocks the code for it costs registers, 1 to 3 us a call).
+template <typename T, int D>
+__device__ __forceinline__ void zero_rows(const qp_kv_attn_args& a, int first, int n)
+{
+    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int row = first; row < a.rows.tokens; row += n) {
+        bool mine = false;
+        for (int b = threadIdx.x; b < a.rows.batch && !mine; b += THREADS) {
+            Seq q;
+            q.pos = qp_kv_ld(a.rows.pos + b);
+            q.row0 = qp_kv_start(a.rows, b);
+            q.n = min(qp_kv_start(a.rows, b + 1) - q.row0, a.max_new);
+            mine = takes_part(q) && row >= q.row0 && row - q.row0 < q.n;
+        }
+        if (__syncthreads_or(mine)) continue;
+        for (int64_t i = threadIdx.x; i < (int64_t)a.q_heads * (D / 4); i += THREADS)
+            put_out(static_cast<T*>(a.out) + row * a.ot + i / (D / 4) * a.oh + 4 * (i % (D / 4)), a.out_vec, zero);
+    }
 }
 
 // What a tile's rows need at the end, worked out once by a thread each: where a row of out begins, and 1 over the sum of its weights (0 for
@@ -434,10 +463,14 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, n = lane >> 2, j = lane & 3;
 
     int b0 = 0;
-    int64_t base = 0, upto = load_chunk<ROWS>(a, 0, 0, chunk), W = upto;
-    for (int c = THREADS; c < a.rows.batch; c += THREADS) W = load_chunk<ROWS>(a, c, W, chunk);
-    const int64_t blocks = (int64_t)gridDim.x * MIN_RUN < W ? (int64_t)gridDim.x : (W + MIN_RUN - 1) / MIN_RUN;
-    if ((int64_t)blockIdx.x >= blocks) return;
+    bool rest = a.rows.batch == 0;
+    int64_t base = 0, upto = load_chunk<ROWS>(a, 0, 0, chunk, &rest), W = upto;
+    for (int c = THREADS; c < a.rows.batch; c += THREADS) W = load_chunk<ROWS>(a, c, W, chunk, &rest);
+    const int64_t most = gridDim.x - REST_BLOCKS, blocks = most * MIN_RUN < W ? most : (W + MIN_RUN - 1) / MIN_RUN;
+    if ((int64_t)blockIdx.x >= blocks) {
+        if (a.zero_rest && __syncthreads_or(rest)) zero_rows<T, D>(a, blockIdx.x - (int)blocks, gridDim.x - (int)blocks);
+        return;
+    }
     const int64_t begin = quotient(blockIdx.x * W, blocks), end = quotient((blockIdx.x + 1ll) * W, blocks);
     if (a.rows.batch > THREADS) {                                // back to the chunk that the run begins in
         upto = load_chunk<ROWS>(a, 0, 0, chunk);
@@ -968,7 +1001,9 @@ extern "C" int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, co
     if (!(h_plan->scale - h_plan->scale == 0.f)) return qp_fail(ctx, QP_ERR_INVALID_ARG, "scale must be finite");
     const int group = h_plan->q_heads / c->heads;
     if ((int64_t)h_batch->tokens * h_plan->q_heads >= (1ll << 31) - 4096) return qp_fail(ctx, QP_ERR_INVALID_ARG, "tokens * q_heads must be below 2^31 - 4096");
-    if (h_batch->batch == 0 || h_batch->tokens == 0 || h_batch->max_new == 0) return QP_OK;
+    if (h_plan->flags & ~QP_KV_ZERO_REST) return qp_fail(ctx, QP_ERR_INVALID_ARG, "flags");
+    const bool zero_rest = (h_plan->flags & QP_KV_ZERO_REST) != 0;
+    if (h_batch->tokens == 0 || (!zero_rest && (h_batch->batch == 0 || h_batch->max_new == 0))) return QP_OK;
     if (!d_q || !d_out) return qp_fail(ctx, QP_ERR_INVALID_ARG, "null d_q or d_out");
     const int64_t es = dtype == QP_F32 ? 4 : 2;
     if ((((uintptr_t)d_q | (uintptr_t)d_out) & (uintptr_t)(es - 1)) || ((uintptr_t)d_lse & 3u)) return qp_fail(ctx, QP_ERR_ALIGNMENT, "d_q, d_out or d_lse");
@@ -995,6 +1030,7 @@ extern "C" int32_t qp_kv_attention(qp_ctx* ctx, const qp_kv_cache_t* h_cache, co
     a.out_vec = (((uintptr_t)d_out & (uintptr_t)(4 * es - 1)) | (uintptr_t)(((out_token_stride | out_head_stride) * es) & (4 * es - 1))) == 0;
     a.count = static_cast<unsigned*>(h_plan->d_work);
     a.part = reinterpret_cast<float*>(a.count + QP_KV_COUNTERS);
+    a.zero_rest = zero_rest;
     a.status = ctx->d_status;
     a.many = 0x7FFFFFFF;
     a.wait_cycles = ctx->wait_cycles;

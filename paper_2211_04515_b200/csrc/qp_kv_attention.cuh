@@ -21,6 +21,7 @@ struct qp_kv_attn_args {
     int64_t ot, oh;
     float* lse;
     bool vec, out_vec;                           // 16-byte loads of q; stores of four elements
+    bool zero_rest;                              // rows that no sequence writes become 0
     unsigned* count;
     float* part;
     unsigned* status;

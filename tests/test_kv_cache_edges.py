@@ -1,5 +1,5 @@
 """The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
-table, more sequences than rows."""
+table, more sequences than rows, rows that no sequence writes."""
 import numpy as np
 import pytest
 import torch
@@ -193,3 +193,65 @@ def test_batches_of_more_sequences_than_rows(ctx, dtype, group):
         for s in range(tokens, 7):
             ids = cache.table[s, :-(-lens[s] // 16)].long()
             assert torch.equal(cache.pool[0, ids], before[0, ids])
+
+
+def poisoned(like):
+    """The next allocation of this size on this stream comes from memory full of NaN."""
+    x = torch.full_like(like, float("nan"))
+    torch.cuda.current_stream().synchronize()
+    del x
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [1, 50])
+def test_new_output_is_zero_where_no_sequence_writes(ctx, dtype, new):
+    rng = np.random.default_rng(21)
+    heads, group, dim, page, lens = 2, 4, 128, 16, [100, 200, 300]
+    cache = make(rng, lens, heads, dim, page)
+    fill(ctx, rng, cache, lens)
+    plan = ctx.qp_kv_attention_plan(cache, heads * group)
+    rows = 4 * new + 9
+    q = torch.from_numpy(rng.standard_normal((rows, heads * group, dim)).astype(np.float32)).cuda().to(dtype)
+
+    def run(pos, start, tokens, max_new=new, slots=None):
+        batch = qp.KVBatch(ints(pos), start=None if start is None else ints(start), tokens=tokens, max_new=max_new,
+                           slots=None if slots is None else ints(slots))
+        kept = ctx.qp_kv_attention(cache, batch, q, plan, out=torch.full_like(q, 5.0))
+        poisoned(q)
+        got = ctx.qp_kv_attention(cache, batch, q, plan)
+        want = torch.where(kept == 5, torch.zeros_like(kept), kept)
+        bits = torch.int16 if dtype == BF16 else torch.int32        # (NaN of rows that were never written are the same too)
+        assert torch.equal(got.view(bits), want.view(bits))
+        assert (kept[tokens:] == 5).all()                           # what a caller gives keeps its rows
+        return kept
+
+    n = new
+    assert (run([50, 120, 200], [0, n, 2 * n, 3 * n], 3 * n)[:3 * n] != 5).all()           # nothing left out but q's last rows
+    kept = run([50, -1, 200], [0, n, 2 * n, 3 * n], 3 * n)                                 # one takes no part
+    assert (kept[n:2 * n] == 5).all() and (kept[2 * n:3 * n] != 5).all()
+    run([-1, -1, -1], [0, n, 2 * n, 3 * n], 3 * n)                                         # nobody does
+    run([50, 120, 200], [3, 3 + n, 3 + n, 3 + 2 * n], 4 * n + 9)                           # rows in front, behind, and an empty sequence
+    run([50, 120], [0, n + 2, 2 * n + 4], 2 * n + 4)                                       # more tokens than max_new
+    run([50, 2 ** 31 - 2], [0, n, 2 * n], 2 * n + 1)                                       # a position past 2^31 - 1 (n > 1), or past the table
+    run([50, 120, 200], None, 3), run([50, -1, 200], None, 3), run([50, 120], None, 4 * n + 9)
+    run([50, 120], [n, n, 0], 2 * n)                                                       # start goes down
+    run([], None, 0), run([], None, 5), run([50], [0, 0], 0), run([50], [0, n], n, 0)      # nothing to do
+    many = 290                                                      # more sequences than a block looks at at a time
+    pos = [50 if b % 3 else -1 for b in range(many)]
+    run(pos, [0] * 200 + [1] * 40 + [2 + n] * (many - 239), 2 + n, slots=[b % 3 for b in range(many)])
+    ctx.qp_get_status()
+
+
+@pytest.mark.gpu
+def test_rows_of_an_exhausted_step_are_zero(ctx):
+    heads, dim = 2, 64
+    cache = qp.KVCache.empty(2, heads, dim, 3, 4, 16)
+    batch = qp.KVBatch(ints([0, 0, 0]))
+    plan = ctx.qp_kv_attention_plan(cache, heads)
+    q = torch.randn(3, heads, dim, device="cuda").to(BF16)
+    ctx.qp_kv_extend(cache, batch)
+    ctx.qp_kv_append(cache, batch, q, q)
+    poisoned(q)
+    assert (ctx.qp_kv_attention(cache, batch, q, plan) == 0).all()
+    assert ctx.qp_get_status() == qp.QP_DEV_KV_EXHAUSTED
