@@ -712,6 +712,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         __syncwarp();
         fence_after();
         const bool out = mine && !given_up(sh);
+        bad = bad && l != 0.f;                                   // (a row that sees nothing is 0, whatever its query)
         float* part = a.part + ((int64_t)s.at * 2 + t) * C::PART;
         const int token = s.row0 + r / a.group, head = s.head * a.group + r % a.group;      // (of a row that is there)
         unsigned short* to = static_cast<unsigned short*>(a.out) + (int64_t)token * a.ot + (int64_t)head * a.oh;

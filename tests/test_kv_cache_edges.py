@@ -1,5 +1,5 @@
 """The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
-table, more sequences than rows, rows that no sequence writes."""
+table, more sequences than rows, rows that no sequence writes, queries that see nothing."""
 import numpy as np
 import pytest
 import torch
@@ -255,3 +255,28 @@ def test_rows_of_an_exhausted_step_are_zero(ctx):
     poisoned(q)
     assert (ctx.qp_kv_attention(cache, batch, q, plan) == 0).all()
     assert ctx.qp_get_status() == qp.QP_DEV_KV_EXHAUSTED
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [1, 80])
+def test_queries_that_see_nothing(ctx, dtype, new):
+    """A row that sees no key is 0 with lse -inf, whatever its query holds; one that sees a key and has a non-finite element is NaN."""
+    rng = np.random.default_rng(22)
+    group, dim, lens = 4, 128, [300, 90 + new]
+    cache = make(rng, lens, 1, dim, 16)
+    fill(ctx, rng, cache, lens)
+    q = torch.from_numpy(rng.standard_normal((2 * new, group, dim)).astype(np.float32)).cuda().to(dtype)
+    q[0, 1, 3] = float("nan")
+    q[0, 2, 5] = float("inf")
+    q[new, 0, 7] = float("nan")
+    q[2 * new - 1, 3, 9] = -float("inf")
+    batch = qp.KVBatch(ints([200, 90]), slots=ints([7, 1]), start=ints([0, new, 2 * new]), tokens=2 * new, max_new=new)   # there is no slot 7
+    plan = ctx.qp_kv_attention_plan(cache, group)
+    lse = torch.empty(2 * new, group, device="cuda")
+    out = ctx.qp_kv_attention(cache, batch, q, plan, out=torch.full_like(q, 5.0), lse=lse)
+    assert ctx.qp_get_status() == qp.QP_DEV_KV_RANGE
+    assert (out[:new] == 0).all() and (lse[:new] == -np.inf).all()
+    bad = ~q[new:].isfinite().all(-1)
+    assert bad.sum() == 2 and out[new:][bad].isnan().all() and lse[new:][bad].isnan().all()
+    assert out[new:][~bad].isfinite().all() and lse[new:][~bad].isfinite().all()
