@@ -571,19 +571,18 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
         for (int t = 0; t < NT; ++t) {
             float top = 0.f, sum = 0.f;
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) { top = fmaxf(top, fabsf(e[t][i])); sum += e[t][i]; }
+            for (int i = 0; i < D / 4; ++i) top = fmaxf(top, fabsf(e[t][i]));
 #pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-                sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            }
-            const bool bad = !(top < __int_as_float(0x7F800000)) || !(fabsf(sum) < __int_as_float(0x7F800000));
+            for (int o = 1; o < 4; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
             // the row's largest element to [2^11, 2^12): fp16 then holds what is down to 2^-25 of it whole
             int ex = 265 - (int)(__float_as_uint(top) >> 23);
             ex = top == 0.f ? 127 : ex > 254 ? 254 : ex;
             const float norm = __uint_as_float((unsigned)ex << 23);
 #pragma unroll
-            for (int i = 0; i < D / 4; ++i) e[t][i] = bad ? 0.f : e[t][i] * norm;
+            for (int i = 0; i < D / 4; ++i) { e[t][i] *= norm; sum += e[t][i]; }      // (at most 2^20; NaN where an element is not finite,
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            if (!(top < __int_as_float(0x7F800000))) sum = __int_as_float(0x7FC00000);   // or taken so; products stay in the query's column)
 #pragma unroll
             for (int w = 0; w < KW; ++w) {
                 const float* x = e[t] + 8 * w;
@@ -595,7 +594,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
                         ql[t][4 * w + i] = half2_of(x[i] * f - half_lo(qb[t][4 * w + i]), x[i + 4] * f - half_hi(qb[t][4 * w + i]));
                 }
             }
-            const float my_kf = a.scale_log2 / norm * (SPLIT ? 1.f : 16777216.f), my_qs = bad ? __int_as_float(0x7FC00000) : sum * a.scale_log2;
+            const float back = a.scale_log2 / norm, my_kf = back * (SPLIT ? 1.f : 16777216.f), my_qs = sum * back;
             kf[t] = qp_pack2(__shfl_sync(0xFFFFFFFFu, my_kf, 8 * j), __shfl_sync(0xFFFFFFFFu, my_kf, 8 * j + 4));
             qs[t] = qp_pack2(__shfl_sync(0xFFFFFFFFu, my_qs, 8 * j), __shfl_sync(0xFFFFFFFFu, my_qs, 8 * j + 4));
         }

@@ -1,5 +1,5 @@
 """The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
-table, more sequences than rows, rows that no sequence writes, queries that see nothing."""
+table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32."""
 import numpy as np
 import pytest
 import torch
@@ -280,3 +280,25 @@ def test_queries_that_see_nothing(ctx, dtype, new):
     bad = ~q[new:].isfinite().all(-1)
     assert bad.sum() == 2 and out[new:][bad].isnan().all() and lse[new:][bad].isnan().all()
     assert out[new:][~bad].isfinite().all() and lse[new:][~bad].isfinite().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,new", [(F32, 1), (BF16, 1), (BF16, 50)])
+def test_queries_whose_sum_passes_fp32(ctx, dtype, new):
+    """The elements are finite and so are the scores: the rows are too."""
+    rng = np.random.default_rng(23)
+    group, dim, n = 4, 128, 200
+    cache = make(rng, [n], 1, dim, 16)
+    fill(ctx, rng, cache, [n])
+    q = torch.from_numpy((np.abs(rng.standard_normal((new, group, dim))) * 5e37).astype(np.float32)).cuda().to(dtype)
+    scale = 1e-38
+    batch = qp.KVBatch(ints([n - new]), start=ints([0, new]), tokens=new, max_new=new)
+    plan = ctx.qp_kv_attention_plan(cache, group, scale=scale)
+    scale = float(np.float32(scale))
+    out = ctx.qp_kv_attention(cache, batch, q, plan).double().cpu().numpy()
+    assert ctx.qp_get_status() == 0
+    k, v = ref.sequence(cache.pool[0].cpu().numpy(), cache.table[0].cpu().numpy(), 0, n, 16, dim)
+    for i in range(new):
+        for g in range(group):
+            want, bound, _ = bound_of(q[i, g].double().cpu().numpy(), k, v, np.arange(n) <= n - new + i, scale, dtype, halves(dtype, dim, new * group))
+            assert (np.abs(out[i, g] - want) <= bound).all()
