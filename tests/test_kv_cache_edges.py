@@ -1,5 +1,5 @@
 """The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
-table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32."""
+table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32, large batches."""
 import numpy as np
 import pytest
 import torch
@@ -302,3 +302,80 @@ def test_queries_whose_sum_passes_fp32(ctx, dtype, new):
         for g in range(group):
             want, bound, _ = bound_of(q[i, g].double().cpu().numpy(), k, v, np.arange(n) <= n - new + i, scale, dtype, halves(dtype, dim, new * group))
             assert (np.abs(out[i, g] - want) <= bound).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attention_of_a_large_batch(ctx, dtype):
+    """More sequences than a block holds at a time (128), runs of work that cross these borders, a long sequence behind the first of them;
+    sequences without tokens and ones that take no part in between."""
+    rng = np.random.default_rng(24)
+    heads, group, dim, page, batch_size = 12, 2, 64, 16, 300
+    lens = [int(x) for x in rng.integers(1, 70, batch_size)]
+    lens[205], lens[290] = 5000, 900
+    cache = make(rng, lens, heads, dim, page)
+    fill(ctx, rng, cache, lens)
+    slots = rng.permutation(batch_size)
+    counts = [int(min(lens[s], rng.choice([0, 1, 1, 1, 2, 5]))) for s in slots]
+    pos = [lens[s] - c if b % 11 else -1 for b, (s, c) in enumerate(zip(slots, counts))]
+    start = np.concatenate(([0], np.cumsum(counts)))
+    total = int(start[-1])
+    q = torch.from_numpy(rng.standard_normal((total, heads * group, dim)).astype(np.float32)).cuda().to(dtype)
+    for window in (0, 100):
+        batch = qp.KVBatch(ints(pos), slots=ints(slots), start=ints(start), tokens=total, max_new=5)
+        plan = ctx.qp_kv_attention_plan(cache, heads * group, window)
+        out, lse = torch.full_like(q, 5.0), torch.full((total, heads * group), 5.0, device="cuda")
+        ctx.qp_kv_attention(cache, batch, q, plan, out=out, lse=lse)
+        assert ctx.qp_get_status() == 0
+        for b in range(batch_size):
+            if pos[b] < 0:
+                assert (out[start[b]:start[b + 1]] == 5).all()
+        check_attention(ctx, cache, lens, slots, pos, start, q, window, out, lse, dim ** -0.5)
+        assert int(plan.work[:4096 * 4].count_nonzero()) == 0
+    # a token each, no start: rows of 300 sequences
+    at = [lens[s] - 1 for s in slots]
+    q1 = torch.from_numpy(rng.standard_normal((batch_size, heads * group, dim)).astype(np.float32)).cuda().to(dtype)
+    plan = ctx.qp_kv_attention_plan(cache, heads * group)
+    lse = torch.empty(batch_size, heads * group, device="cuda")
+    out = ctx.qp_kv_attention(cache, qp.KVBatch(ints(at), slots=ints(slots)), q1, plan, lse=lse)
+    check_attention(ctx, cache, lens, slots, at, np.arange(batch_size + 1), q1, 0, out, lse, dim ** -0.5)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dim", [64, 128])
+def test_chunks_of_a_large_batch(ctx, dim):
+    """More than 32 sequences with 160 or more query rows, more parts of items to a block than its list holds (32), sequences of the other
+    kernel among them."""
+    rng = np.random.default_rng(25)
+    heads, group, page = 120, 4, 16
+    lens = [int(x) for x in rng.integers(45, 130, 46)]
+    counts = [int(x) for x in rng.integers(40, 45, 46)]
+    counts[3], counts[20], counts[44] = 1, 0, 7
+    cache = make(rng, lens, heads, dim, page)
+    fill(ctx, rng, cache, lens, dtype=BF16)
+    pos = [n - c for n, c in zip(lens, counts)]
+    pos[10] = -1
+    start = np.concatenate(([0], np.cumsum(counts)))
+    total = int(start[-1])
+    q = torch.from_numpy(rng.standard_normal((total, heads * group, dim), dtype=np.float32)).cuda().to(BF16)
+    batch = qp.KVBatch(ints(pos), start=ints(start), tokens=total, max_new=max(counts))
+    plan = ctx.qp_kv_attention_plan(cache, heads * group)
+    out, lse = torch.full_like(q, 5.0), torch.full((total, heads * group), 5.0, device="cuda")
+    ctx.qp_kv_attention(cache, batch, q, plan, out=out, lse=lse)
+    assert ctx.qp_get_status() == 0 and int(plan.work[:4096 * 4].count_nonzero()) == 0
+    assert (out[start[10]:start[11]] == 5).all()
+    pool, table = cache.pool[0].cpu().numpy(), cache.table.cpu().numpy()
+    on, ln, qn = out.double().cpu().numpy(), lse.double().cpu().numpy(), q.double().cpu().numpy()
+    written = np.ones(total, bool)
+    written[start[10]:start[11]] = False
+    assert np.isfinite(on).all() and (np.abs(on[written]).max(-1) < 5).mean() > 0.9
+    for b in range(46):
+        if pos[b] < 0 or counts[b] == 0:
+            continue
+        for _ in range(12):
+            i, hq = int(rng.integers(counts[b])), int(rng.integers(heads * group))
+            k, v = ref.sequence(pool, table[b], hq // group, lens[b], page, dim)
+            row = int(start[b]) + i
+            want, e, bound, lb = ref.attention_row(qn[row, hq], k, v, np.arange(lens[b]) <= pos[b] + i, dim ** -0.5, 2.0 ** -11, torch.finfo(BF16).eps / 2,
+                                                   halves(BF16, dim, counts[b] * group))
+            assert (np.abs(on[row, hq] - want) <= bound).all() and abs(ln[row, hq] - e) <= lb
