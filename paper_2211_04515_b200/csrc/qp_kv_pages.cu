@@ -540,8 +540,11 @@ extern "C" int32_t qp_kv_fork(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const i
     const Cache c = cache_of(ctx, h_cache);
     const Moves m = moves_of(h_cache, c);
     qp_kv_launch(kv_fork_plan_kernel, 1u, PLAN, 0, s, c, d_src, d_dst, n);
+    ctx->launches += 1;
+    rc = qp_check_launch(ctx, "qp_kv_fork");
+    if (rc) return rc;                                           // (lists that nobody has written are not gone by)
     qp_kv_launch(kv_fork_kernel, (unsigned)(move_grid(ctx, n + (int64_t)n * m.layers * m.chunks)), MOVE_THREADS, 0, s, c, m, d_src, d_dst, n);
-    ctx->launches += 2;
+    ctx->launches += 1;
     return qp_check_launch(ctx, "qp_kv_fork");
 }
 
@@ -559,8 +562,11 @@ extern "C" int32_t qp_kv_copy_pages(qp_ctx* ctx, const qp_kv_cache_t* h_cache, c
     const Moves m = moves_of(h_cache, c);
     const bool in_shared = h_cache->num_pages <= SMEM_PAGES;
     qp_kv_launch(kv_copy_plan_kernel, 1u, PLAN, in_shared ? (size_t)h_cache->num_pages * 4 : 0, s, c, d_src, d_dst, n, in_shared);
+    ctx->launches += 1;
+    rc = qp_check_launch(ctx, "qp_kv_copy_pages");
+    if (rc) return rc;
     qp_kv_launch(kv_move_kernel, (unsigned)(move_grid(ctx, (int64_t)n * m.layers * m.chunks)), MOVE_THREADS, 0, s, m, n);
-    ctx->launches += 2;
+    ctx->launches += 1;
     return qp_check_launch(ctx, "qp_kv_copy_pages");
 }
 
@@ -575,7 +581,10 @@ extern "C" int32_t qp_kv_compact(qp_ctx* ctx, const qp_kv_cache_t* h_cache, int3
     const Cache c = cache_of(ctx, h_cache);
     const Moves m = moves_of(h_cache, c);
     qp_kv_launch(kv_compact_plan_kernel, 1u, PLAN, 0, s, c, d_live);
+    ctx->launches += 1;
+    rc = qp_check_launch(ctx, "qp_kv_compact");
+    if (rc) return rc;
     qp_kv_launch(kv_compact_kernel, (unsigned)(move_grid(ctx, (int64_t)h_cache->num_pages * m.layers * m.chunks)), MOVE_THREADS, 0, s, c, m);
-    ctx->launches += 2;
+    ctx->launches += 1;
     return qp_check_launch(ctx, "qp_kv_compact");
 }

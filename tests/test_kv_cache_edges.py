@@ -1,5 +1,6 @@
 """The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
-table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32, large batches."""
+table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32, large batches,
+launches that are refused."""
 import numpy as np
 import pytest
 import torch
@@ -49,6 +50,22 @@ def bound_of(q, k, v, seen, scale, dtype, in_halves):
     err = same + moved(2 * ds) + v_off
     half = torch.finfo(dtype).eps / 2
     return out, err + half * (np.abs(out) + err), 2 * (same + half * (np.abs(out) + err))
+
+
+def test_a_refused_launch_is_the_last(tmp_path):
+    """A page call whose deciding launch is refused returns the error and starts no move: shown over a runtime of the test's own."""
+    import os
+    import subprocess
+    from paper_2211_04515_b200 import build
+    nvcc = build._nvcc()
+    obj, out = str(tmp_path / "pages.o"), str(tmp_path / "refused")
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc))), "include")
+    subprocess.run([nvcc, "-c", *build.NVCC_FLAGS[1:], "-I", build.INCLUDE, "-I", build.CSRC, "-o", obj,
+                    os.path.join(build.CSRC, "qp_kv_pages.cu")], check=True)
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-I", build.INCLUDE, "-I", build.CSRC, "-I", cuda, "-o", out,
+                    os.path.join(build.ROOT, "tests", "c_abi", "kv_refused_launch.cpp"), obj], check=True)
+    run = subprocess.run([out], capture_output=True, text=True, timeout=60)
+    assert run.returncode == 0 and run.stdout.strip() == "ok", run.stderr
 
 
 OUTLIERS = [
