@@ -229,7 +229,7 @@ __device__ __forceinline__ void find_part(const qp_kv_attn_args& a, const Chunk&
         if (in) { hit = in; at = 32 * k; }
     }
     at += __ffs(hit) - 1;
-    const int4 x = sh.seq[at];
+    const int4 x = sh.seq[QP_CK(at, THREADS)];
     Part p;
     p.q.pos = x.x; p.q.n = x.y; p.q.row0 = x.z; p.q.slot = x.w;
     derive<ROWS>(a, p.q);
@@ -383,11 +383,11 @@ __device__ __forceinline__ void add_parts(const qp_kv_attn_args& a, const Seq& q
                                           int step, int n, float* sum, char* smem, RowEnds& ends)
 {
     constexpr int PART = ROWS * (D + 2);
-    auto part = [&](int i) { return a.part + (int64_t)(i ? even + 2 * step * i : at) * PART; };
+    auto part = [&](int i) { return a.part + (int64_t)QP_CK(i ? even + 2 * step * i : at, 2 * gridDim.x) * PART; };
     float* f = reinterpret_cast<float*>(smem);                   // [n][2 ROWS] references, then factors, and sums; [ROWS] of the whole
     float* tops = f + n * 2 * ROWS;
     __syncthreads();                                             // shared memory is free
-    for (int i = threadIdx.x; i < n * 2 * ROWS; i += THREADS) f[i] = __ldcg(part(i / (2 * ROWS)) + ROWS * D + i % (2 * ROWS));
+    for (int i = threadIdx.x; i < n * 2 * ROWS; i += THREADS) f[QP_CK(i, WARPS * ROWS * (D + 2) - 2 * ROWS)] = __ldcg(part(i / (2 * ROWS)) + ROWS * D + i % (2 * ROWS));
     __syncthreads();
     if (threadIdx.x < (unsigned)rows) {
         const int r = threadIdx.x;
@@ -536,9 +536,9 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             if (i < count * SL) {
                 if ((i & 31) == 0 && i > 0) place = place_of(p, i >> 5, ask(p, i >> 5));
                 const int64_t from = __shfl_sync(0xFFFFFFFFu, place, i & 31);
-                if (lane == 0) sh_ok[warp][put] = from >= 0;
+                if (lane == 0) sh_ok[warp][QP_CK(put, STAGES)] = from >= 0;
                 if (from >= 0) {
-                    char* to = ring + put * SB + lane * 16;
+                    char* to = ring + QP_CK(put, STAGES) * SB + lane * 16;
                     const char* src = a.pool + from + lane * 16;
 #pragma unroll
                     for (int c = 0; c < SB / 512; ++c) copy16(to + 512 * c, src + 512 * c);
@@ -625,7 +625,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             bool ok[SL], all = t0 >= all_lo && t0 + SL * QP_KV_SLICE <= all_hi;
 #pragma unroll
             for (int i = 0; i < SL; ++i) {
-                at[i] = ring + take * SB;
+                at[i] = ring + QP_CK(take, STAGES) * SB;
                 ok[i] = sh_ok[warp][take] != 0;
                 all = all && ok[i];
                 take = take + 1 == STAGES ? 0 : take + 1;
@@ -893,7 +893,7 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             // a block's part of an item is its first if the item began in front of it or with it
             at = 2 * (int)blockIdx.x + (p.u == begin ? 0 : 1);
         }
-        float* mine_at = a.part + (int64_t)at * C::PART;
+        float* mine_at = a.part + (int64_t)QP_CK(at, 2 * gridDim.x) * C::PART;
         if (threadIdx.x < (unsigned)rows) {                      // the warps' references become factors
             const int r = threadIdx.x;
             float top = mm[r], sl = 0.f;
@@ -932,13 +932,13 @@ __global__ void __launch_bounds__(THREADS, Cfg<D, NT, SPLIT>::PER_SM) kv_attn_ke
             const int group = ((int)blockIdx.x - c0) / step, groups = (parts + step - 1) / step;
             const int gc = c0 + group * step, gn = parts - group * step < step ? parts - group * step : step;
             const int g_at = group ? 2 * gc : first_at;
-            float* sum = a.part + (int64_t)g_at * C::PART;
-            bool mine = arrived(a.count + g_at, gn, sh_last);
+            float* sum = a.part + (int64_t)QP_CK(g_at, 2 * gridDim.x) * C::PART;
+            bool mine = arrived(a.count + QP_CK(g_at, QP_KV_COUNTERS / 2), gn, sh_last);
             if (mine && groups == 1) {
                 add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, 1, parts, nullptr, smem, ends);
             } else if (mine) {
                 add_parts<T, D, ROWS>(a, q, head, tile, rows, g_at, 2 * gc, 1, gn, sum, smem, ends);
-                mine = arrived(a.count + QP_KV_COUNTERS / 2 + first_at, groups, sh_last);
+                mine = arrived(a.count + QP_KV_COUNTERS / 2 + QP_CK(first_at, QP_KV_COUNTERS / 2), groups, sh_last);
                 if (mine) add_parts<T, D, ROWS>(a, q, head, tile, rows, first_at, 2 * c0, step, groups, nullptr, smem, ends);
             }
         }

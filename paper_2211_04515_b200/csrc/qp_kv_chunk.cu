@@ -285,7 +285,7 @@ __device__ __forceinline__ void list_parts(const qp_kv_attn_args& a, Shared& sh,
                         s.first_at = 2 * s.c0 + ((int64_t)s.c0 * W / blocks < i0 ? 1 : 0);
                         s.at = 2 * (int)blockIdx.x + (u == begin ? 0 : 1);
                     }
-                    if ((threadIdx.x & 31) == 0) sh.segs[n] = s;
+                    if ((threadIdx.x & 31) == 0) sh.segs[QP_CK(n, SEGS)] = s;
                     ++n;
                 }
                 u += g1 - g0;
@@ -399,7 +399,7 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
 #pragma unroll
                 for (int l = 0; l < L; ++l) {
                     const int sl = (l * 128 + p) / PER, key = sl * QP_KV_SLICE + row;
-                    const float2 q = sh.quant[st][h][key];
+                    const float2 q = sh.quant[st][h][QP_CK(key, TILE)];
                     const float sc = q.y * f;
                     const unsigned m1 = half2_of(sc, sc), m16 = mul_h2(m1, 0x2C002C00u);         // (times 2^-4)
                     const float mid = fmaf(8.f, sc, q.x * f);
@@ -713,7 +713,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         fence_after();
         const bool out = mine && !given_up(sh);
         bad = bad && l != 0.f;                                   // (a row that sees nothing is 0, whatever its query)
-        float* part = a.part + ((int64_t)s.at * 2 + t) * C::PART;
+        float* part = a.part + ((int64_t)QP_CK(s.at, 2 * gridDim.x) * 2 + t) * C::PART;
         const int token = s.row0 + r / a.group, head = s.head * a.group + r % a.group;      // (of a row that is there)
         unsigned short* to = static_cast<unsigned short*>(a.out) + (int64_t)token * a.ot + (int64_t)head * a.oh;
         const float un = ex2(X - m - (float)P_SHIFT), over = s.split ? 1.f : l == 0.f ? 0.f : 1.f / l;
@@ -744,14 +744,14 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
             __threadfence();
             group_sync(2 + t);
             if (row == 0) {
-                unsigned* count = a.count + s.first_at * 2 + t;
+                unsigned* count = a.count + QP_CK(s.first_at * 2 + t, QP_KV_COUNTERS);
                 sh.last[t] = atomicAdd(count, 1u) == (unsigned)(parts - 1);
                 if (sh.last[t]) *count = 0u;
             }
             group_sync(2 + t);
             if (__all_sync(0xFFFFFFFFu, sh.last[t] != 0 && !given_up(sh))) {
                 __threadfence();
-                auto at = [&](int p) { return a.part + ((int64_t)(p ? 2 * (s.c0 + p) : s.first_at) * 2 + t) * C::PART; };
+                auto at = [&](int p) { return a.part + ((int64_t)QP_CK(p ? 2 * (s.c0 + p) : s.first_at, 2 * gridDim.x) * 2 + t) * C::PART; };
                 const int warp_row = row & ~31, base_row = s.tile * ROWS + t * TILE;
                 // a lane's row: the parts' weights, and the sum of their sums
                 float best = M_NONE, sl = 0.f;

@@ -108,7 +108,7 @@ __device__ __forceinline__ volatile int* claim_slots(const Cache& c, const int32
     volatile int* claim = c.max_seqs <= SMEM_CLAIMS ? sh_claim : c.s0;
     for (int i = threadIdx.x; i < n; i += PLAN) {
         const int s = qp_kv_ld(slots + i);
-        if (s >= 0 && s < c.max_seqs) claim[s] = NONE;
+        if (s >= 0 && s < c.max_seqs) claim[QP_CK(s, c.max_seqs <= SMEM_CLAIMS ? SMEM_CLAIMS : c.max_seqs)] = NONE;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += PLAN) {
@@ -160,14 +160,14 @@ __global__ void __launch_bounds__(PLAN) kv_extend_kernel(const Cache c, const in
             if (total > c.num_pages >> 11) { wanted = c.num_pages + 1; break; }
         }
         const int at = wanted + block_scan(need, sh, total);
-        if (b < batch) { c.s1[b] = at; c.s2[b] = old; }
+        if (b < batch) { c.s1[QP_CK(b, c.max_seqs)] = at; c.s2[QP_CK(b, c.max_seqs)] = old; }
         wanted += total;                                         // (at most 2^29 before, 2^29 + 2^21 added)
         if (wanted > c.num_pages) break;                         // uniform
     }
     int* taken = wanted <= SMEM_TAKEN ? sh_taken : c.a;
     int found = 0;
     if (wanted <= c.num_pages)
-        found = for_pages(c, 0, wanted, sh, [](int, int refs) { return refs == 0; }, [&](int r, int p) { taken[r] = p; });
+        found = for_pages(c, 0, wanted, sh, [](int, int refs) { return refs == 0; }, [&](int r, int p) { taken[QP_CK(r, wanted <= SMEM_TAKEN ? SMEM_TAKEN : c.num_pages)] = p; });
     __syncthreads();
     if (found < wanted) {
         for (int b = threadIdx.x; b < batch; b += PLAN) pos[b] = -1;
@@ -180,8 +180,8 @@ __global__ void __launch_bounds__(PLAN) kv_extend_kernel(const Cache c, const in
                 if (c.s1[mid] <= k) lo = mid; else hi = mid;
             }
             const int s = slots ? qp_kv_ld(slots + lo) : lo;
-            c.table[(size_t)s * c.max_pages + pages_of(c.s2[lo], c.page_size) + (k - c.s1[lo])] = taken[k];
-            c.refs[taken[k]] = 1;
+            c.table[(size_t)s * c.max_pages + QP_CK(pages_of(c.s2[lo], c.page_size) + (k - c.s1[lo]), c.max_pages)] = taken[k];
+            c.refs[QP_CK(taken[k], c.num_pages)] = 1;
         }
         for (int b = threadIdx.x; b < batch; b += PLAN) {
             const int old = c.s2[b];
@@ -313,12 +313,12 @@ __global__ void __launch_bounds__(PLAN) kv_fork_plan_kernel(const Cache c, const
         }
         int total;
         const int at = wanted + block_scan(tail, sh, total);
-        if (i < n) { c.s1[i] = tail ? at : -1; c.s2[i] = len; }
+        if (i < n) { c.s1[QP_CK(i, c.max_seqs)] = tail ? at : -1; c.s2[QP_CK(i, c.max_seqs)] = len; }
         wanted += total;
     }
     // the pages for the copies into list c, then to the pairs
     const int found = wanted <= c.num_pages
-                          ? for_pages(c, 0, wanted, sh, [](int, int refs) { return refs == 0; }, [&](int r, int p) { c.c[r] = p; })
+                          ? for_pages(c, 0, wanted, sh, [](int, int refs) { return refs == 0; }, [&](int r, int p) { c.c[QP_CK(r, c.num_pages)] = p; })
                           : 0;
     __syncthreads();
     const bool enough = found >= wanted;
@@ -328,8 +328,8 @@ __global__ void __launch_bounds__(PLAN) kv_fork_plan_kernel(const Cache c, const
         if (len < 0) continue;
         c.lens[qp_kv_ld(dst + i)] = len;                            // (the lengths were all read above)
         if (at >= 0) {
-            const int p = c.c[at];
-            c.refs[p] = 1;
+            const int p = c.c[QP_CK(at, c.num_pages)];
+            c.refs[QP_CK(p, c.num_pages)] = 1;
             c.s1[i] = p;
         }
     }
@@ -382,7 +382,7 @@ __global__ void __launch_bounds__(PLAN) kv_copy_plan_kernel(const Cache c, const
     auto ok = [&](int p) { return p >= 0 && p < c.num_pages; };
     for (int i = threadIdx.x; i < n; i += PLAN) {
         const int s = qp_kv_ld(src + i), d = qp_kv_ld(dst + i);
-        if (ok(s) && ok(d)) claim[s] = claim[d] = NONE;
+        if (ok(s) && ok(d)) claim[QP_CK(s, c.num_pages)] = claim[QP_CK(d, c.num_pages)] = NONE;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += PLAN) {
@@ -395,8 +395,8 @@ __global__ void __launch_bounds__(PLAN) kv_copy_plan_kernel(const Cache c, const
         const int s = qp_kv_ld(src + i), d = qp_kv_ld(dst + i);
         const bool good = ok(s) && ok(d) && claim[d] == i && (s == d || claim[s] == NONE);
         range |= !good;
-        c.a[i] = good && s != d ? s : -1;
-        c.b[i] = d;
+        c.a[QP_CK(i, c.num_pages)] = good && s != d ? s : -1;
+        c.b[QP_CK(i, c.num_pages)] = d;
     }
     if (range) atomicOr(c.status, QP_DEV_KV_RANGE);
 }
@@ -428,7 +428,7 @@ __global__ void __launch_bounds__(PLAN) kv_compact_plan_kernel(const Cache c, in
         int rank = at & 0xFFFF;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            if (holes[i] >> lane & 1u) sh_hole[rank + __popc(holes[i] & below)] = p0 + 32 * i;
+            if (holes[i] >> lane & 1u) sh_hole[QP_CK(rank + __popc(holes[i] & below), PER * PLAN / 2)] = p0 + 32 * i;
             rank += __popc(holes[i]);
         }
         __syncthreads();
@@ -437,11 +437,11 @@ __global__ void __launch_bounds__(PLAN) kv_compact_plan_kernel(const Cache c, in
         for (int i = 0; i < PER; ++i) {
             const int p = p0 + 32 * i;
             if (movers[i] >> lane & 1u) {
-                const int k = rank + __popc(movers[i] & below), to = sh_hole[k];
-                c.a[k] = p;
+                const int k = QP_CK(rank + __popc(movers[i] & below), PER * PLAN / 2), to = sh_hole[k];
+                c.a[QP_CK(k, c.num_pages)] = p;
                 c.b[k] = to;
                 c.c[p] = to;
-                c.refs[to] = refs[i];
+                c.refs[QP_CK(to, c.num_pages)] = refs[i];
                 c.refs[p] = 0;
             } else if (p >= live && p < c.num_pages) {
                 c.c[p] = -1;
@@ -456,14 +456,14 @@ __global__ void __launch_bounds__(PLAN) kv_compact_plan_kernel(const Cache c, in
         return;
     }
     const int live = for_pages(c, 0, c.num_pages, sh, [](int, int refs) { return refs != 0; }, [](int, int) {});
-    const int holes = for_pages(c, 0, c.num_pages, sh, [&](int p, int refs) { return p < live && refs == 0; }, [&](int r, int p) { c.b[r] = p; });
+    const int holes = for_pages(c, 0, c.num_pages, sh, [&](int p, int refs) { return p < live && refs == 0; }, [&](int r, int p) { c.b[QP_CK(r, c.num_pages)] = p; });
     // every page at or above `live` has an entry in list c: where it goes, -1 for a free one
     for (int p = live + threadIdx.x; p < c.num_pages; p += PLAN) c.c[p] = -1;
     __syncthreads();
-    for_pages(c, 0, c.num_pages, sh, [&](int p, int refs) { return p >= live && refs != 0; }, [&](int r, int p) { c.a[r] = p; });
+    for_pages(c, 0, c.num_pages, sh, [&](int p, int refs) { return p >= live && refs != 0; }, [&](int r, int p) { c.a[QP_CK(r, c.num_pages)] = p; });
     __syncthreads();
     for (int k = threadIdx.x; k < holes; k += PLAN) {            // as many used pages above as holes below
-        const int from = c.a[k], to = c.b[k];
+        const int from = QP_CK(c.a[k], c.num_pages), to = QP_CK(c.b[k], c.num_pages);
         c.c[from] = to;
         c.refs[to] = c.refs[from];
         c.refs[from] = 0;
@@ -485,7 +485,7 @@ __global__ void __launch_bounds__(MOVE_THREADS) kv_compact_kernel(const Cache c,
     const int64_t entries = (int64_t)c.max_seqs * c.max_pages;
     for (int64_t e = (int64_t)blockIdx.x * MOVE_THREADS + threadIdx.x; e < entries; e += (int64_t)gridDim.x * MOVE_THREADS) {
         const int p = c.table[e];
-        if (p >= live && p < c.num_pages) c.table[e] = c.c[p];
+        if (p >= live && p < c.num_pages) c.table[e] = c.c[QP_CK(p, c.num_pages)];
     }
 }
 

@@ -286,8 +286,8 @@ __global__ void __launch_bounds__(QP_THREADS) kv_append_kernel(const RowArgs a, 
             if (threadIdx.x < 32) look_up<D>(a, first, n, places, flag);
             __syncthreads();
         }
-        const int64_t place = i < pairs ? places.at[in] : -1;
-        const int row = i < pairs ? places.row[in] : 0;
+        const int64_t place = i < pairs ? places.at[QP_CK(in, TOKENS)] : -1;
+        const int row = i < pairs ? places.row[QP_CK(in, TOKENS)] : 0;
         char* s = a.pool + place + (int64_t)head * a.slices * S::BYTES;
         float k_mn, k_mx, v_mn, v_mx, scale[2], inv[2];
         const bool k_fine = ends_of(k, k_mn, k_mx), v_fine = ends_of(v, v_mn, v_mx);
@@ -361,8 +361,8 @@ __global__ void __launch_bounds__(QP_THREADS) kv_gather_kernel(const RowArgs a, 
     __syncthreads();
 #pragma unroll 2
     for (int i = group; i < pairs; i += GROUPS) {
-        const int in = i / a.heads, head = i - in * a.heads, row = places.row[in];
-        const int64_t token = first + in, place = places.at[in];
+        const int in = i / a.heads, head = i - in * a.heads, row = places.row[QP_CK(in, TOKENS)];
+        const int64_t token = first + in, place = places.at[QP_CK(in, TOKENS)];
         if (place < 0) continue;
         const char* s = a.pool + place + (int64_t)head * a.slices * S::BYTES;
         unsigned kw[E / 4], vw[E / 4];

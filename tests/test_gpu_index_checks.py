@@ -38,3 +38,19 @@ def test_small_cases_run_clean_under_the_index_checked_build():
     tail = (run.stdout or "")[-3000:] + (run.stderr or "")[-2000:]
     assert run.returncode == 0, tail
     assert " passed" in run.stdout and "index checks: on, no index out of range" in run.stdout, tail
+
+
+# rows in and out, every shape of attention, random page calls, batches larger than the kernels' tables, rows that nobody writes
+CACHE = ("append_and_gather or (test_attention and not attention_of) or long_sequence or odd_batches or mixed or pages_against or exhausted or more_tokens or "
+         "captured or large_batch or new_output or many_sizes")
+
+
+def test_the_cache_runs_clean_under_the_index_checked_build():
+    from paper_2211_04515_b200 import build
+    lib = build.build(check=True)
+    env = dict(os.environ, QUANTPIPE_LIB=lib)
+    run = subprocess.run([sys.executable, "-m", "pytest", "tests/test_kv_cache.py", "tests/test_kv_cache_edges.py", "-m", "gpu", "-q", "-x", "-k", CACHE],
+                         cwd=ROOT, env=env, capture_output=True, text=True, timeout=1500)
+    tail = (run.stdout or "")[-3000:] + (run.stderr or "")[-2000:]
+    assert run.returncode == 0, tail
+    assert " passed" in run.stdout and "index checks: on, no index out of range" in run.stdout, tail

@@ -68,6 +68,17 @@ def test_a_refused_launch_is_the_last(tmp_path):
     assert run.returncode == 0 and run.stdout.strip() == "ok", run.stderr
 
 
+def test_every_registered_unit_has_index_checks():
+    """The header promises checked indexes in the debug build of every unit that registers for them."""
+    import glob
+    import os
+    from paper_2211_04515_b200 import build
+    units = {os.path.basename(p): open(p).read() for p in glob.glob(os.path.join(build.CSRC, "*.cu"))}
+    registered = [n for n, text in units.items() if "\nQP_CK_UNIT" in text]
+    assert [n for n in units if n.startswith("qp_kv_") and n not in registered] == []
+    assert [n for n in registered if "QP_CK(" not in units[n]] == []
+
+
 OUTLIERS = [
     # dim, dtype, group, new, window
     (128, BF16, 4, 1, 0), (128, F32, 4, 1, 0), (64, F32, 1, 1, 0), (256, BF16, 2, 1, 0), (256, F32, 3, 4, 0),
