@@ -385,6 +385,13 @@ def _ints(t: torch.Tensor, what: str, index: int, n: int | None = None) -> int:
     return got
 
 
+def _int32(v: int, what: str) -> int:
+    """v, for a field of 32 bits (which ctypes would cut to them without a word)."""
+    if not -2**31 <= v < 2**31:
+        raise QuantPipeError(QP_ERR_INVALID_ARG, f"{what} {v} passes 32 bits")
+    return v
+
+
 class KVCache:
     """Keys and values of many sequences in 4 bits, in pages that one block table names for all layers.
 
@@ -407,6 +414,8 @@ class KVCache:
         self.pool, self.table, self.lens, self.refs, self.head_dim = pool, table, lens, refs, head_dim
         self.device, self.layers, self.pages, self.heads, self.page_size = pool.device, layers, pages, heads, 16 * slices
         self.slots, self.max_pages = table.shape
+        for what in ("layers", "pages", "heads", "page_size", "slots", "max_pages"):
+            _int32(getattr(self, what), what)
         work = int(load().qp_kv_work_ints(pages, self.slots))
         self.work = torch.empty(max(work, 1), dtype=torch.int32, device=pool.device)
         self._desc = KVCacheDesc(pool.data_ptr(), pool.stride(0) if layers > 1 else 0, table.data_ptr(), lens.data_ptr(),
@@ -442,7 +451,8 @@ class KVBatch:
             if tokens is None or max_new is None:
                 raise QuantPipeError(QP_ERR_INVALID_ARG, "tokens and max_new are needed with start")
         self.pos, self.slots, self.start = pos, slots, start
-        self.batch, self.tokens, self.max_new = n, n if tokens is None else tokens, 1 if max_new is None else max_new
+        self.batch, self.tokens, self.max_new = (_int32(n, "batch"), _int32(n if tokens is None else tokens, "tokens"),
+                                                 _int32(1 if max_new is None else max_new, "max_new"))
         self._desc = KVBatchDesc(None if slots is None else slots.data_ptr(), None if start is None else start.data_ptr(),
                                  pos.data_ptr(), self.batch, self.tokens, self.max_new, 0)
         self._at = C.addressof(self._desc)
@@ -452,7 +462,7 @@ class KVAttention:
     """What attention over a cache keeps from call to call: its workspace (of one stream at a time) and its constants."""
 
     def __init__(self, work: torch.Tensor, q_heads: int, window: int, scale: float):
-        self.work, self.q_heads, self.window, self.scale = work, q_heads, window, scale
+        self.work, self.q_heads, self.window, self.scale = work, _int32(q_heads, "q_heads"), _int32(window, "window"), scale
         self._index = work.get_device()
         self._desc = KVAttentionDesc(work.data_ptr(), work.nbytes, q_heads, window, scale, 0)
         self._at = C.addressof(self._desc)
@@ -741,6 +751,12 @@ class Context:
             if p._index != self._index:
                 raise QuantPipeError(QP_ERR_INVALID_ARG, f"a cache, batch or plan on cuda:{p._index}, the context on {self.device}")
 
+    @staticmethod
+    def _kv_layer(cache: KVCache, layer: int) -> int:
+        if not 0 <= layer < cache.layers:
+            raise QuantPipeError(QP_ERR_INVALID_ARG, f"layer {layer} of {cache.layers}")
+        return layer
+
     def qp_kv_extend(self, cache: KVCache, batch: KVBatch) -> torch.Tensor:
         """Pages for the batch's new tokens; fills and returns batch.pos and adds to cache.lens."""
         self._kv_here(cache, batch)
@@ -754,7 +770,7 @@ class Context:
         v_code, vt, vh = self._kv_rows(v, batch.tokens, cache.heads, cache.head_dim, "v")
         if code != v_code:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "k and v of different types")
-        self._run("qp_kv_append", cache._at, batch._at, layer, k, v, code, kt, kh, vt, vh)
+        self._run("qp_kv_append", cache._at, batch._at, self._kv_layer(cache, layer), k, v, code, kt, kh, vt, vh)
 
     def qp_kv_gather(self, cache: KVCache, batch: KVBatch, k: torch.Tensor | None = None, v: torch.Tensor | None = None,
                      layer: int = 0, out_dtype: torch.dtype = torch.float32):
@@ -766,7 +782,7 @@ class Context:
         v_code, vt, vh = (code, 0, 0) if v is None else self._kv_rows(v, batch.tokens, cache.heads, cache.head_dim, "v")
         if code is not None and code != v_code:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "k and v of different types")
-        self._run("qp_kv_gather", cache._at, batch._at, layer, k, v, v_code, kt, kh, vt, vh)
+        self._run("qp_kv_gather", cache._at, batch._at, self._kv_layer(cache, layer), k, v, v_code, kt, kh, vt, vh)
         return k, v
 
     def qp_kv_attention_plan(self, cache: KVCache, q_heads: int, window: int = 0, scale: float | None = None) -> KVAttention:
@@ -793,7 +809,7 @@ class Context:
         if lse is not None and not (lse.dtype == torch.float32 and lse.get_device() == self._index and lse.is_contiguous()
                                     and lse.numel() >= batch.tokens * plan.q_heads):
             raise QuantPipeError(QP_ERR_INVALID_ARG, "lse must be a contiguous float32 tensor [tokens, q_heads]")
-        self._run("qp_kv_attention", cache._at, batch._at, at, layer, q, code, qt, qh, out, ot, oh, lse)
+        self._run("qp_kv_attention", cache._at, batch._at, at, self._kv_layer(cache, layer), q, code, qt, qh, out, ot, oh, lse)
         return out
 
     def qp_kv_fork(self, cache: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:

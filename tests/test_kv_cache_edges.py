@@ -1,6 +1,6 @@
 """The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
 table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32, large batches,
-launches that are refused."""
+launches that are refused, numbers past 32 bits."""
 import numpy as np
 import pytest
 import torch
@@ -77,6 +77,15 @@ def test_every_registered_unit_has_index_checks():
     registered = [n for n, text in units.items() if "\nQP_CK_UNIT" in text]
     assert [n for n in units if n.startswith("qp_kv_") and n not in registered] == []
     assert [n for n in registered if "QP_CK(" not in units[n]] == []
+
+
+def test_numbers_past_32_bits_are_refused_on_the_host(lib):
+    work = torch.zeros(16, dtype=torch.uint8)
+    for more in (2**31, 2**32, 2**32 + 7, -2**31 - 1):
+        for q_heads, window in ((4, more), (more, 0)):
+            with pytest.raises(qp.QuantPipeError):
+                qp.KVAttention(work, q_heads, window, 1.0)
+    assert qp.KVAttention(work, 4, 2**31 - 1, 1.0)._desc.window == 2**31 - 1
 
 
 OUTLIERS = [
@@ -330,6 +339,31 @@ def test_queries_whose_sum_passes_fp32(ctx, dtype, new):
         for g in range(group):
             want, bound, _ = bound_of(q[i, g].double().cpu().numpy(), k, v, np.arange(n) <= n - new + i, scale, dtype, halves(dtype, dim, new * group))
             assert (np.abs(out[i, g] - want) <= bound).all()
+
+
+@pytest.mark.gpu
+def test_refusals_of_numbers(ctx):
+    """Sizes, layers and windows past 32 bits, unknown flags: an error, not the number's low bits."""
+    import ctypes as C
+    cache = make(np.random.default_rng(0), [40, 3], 2, 64, 16)
+    pos = ints([0, 0])
+    for more in (2**31, 2**32 + 2):
+        for sizes in (dict(tokens=more), dict(max_new=more), dict(start=ints([0, 1, 2]), tokens=2, max_new=more)):
+            with pytest.raises(qp.QuantPipeError):
+                qp.KVBatch(pos, **sizes)
+    batch, plan = qp.KVBatch(pos), ctx.qp_kv_attention_plan(cache, 4)
+    q, k = torch.zeros(2, 4, 64, device="cuda"), torch.zeros(2, 2, 64, device="cuda")
+    for call, args in ((ctx.qp_kv_append, (k, k)), (ctx.qp_kv_gather, (k, k)), (ctx.qp_kv_attention, (q, plan))):
+        for layer in (1, -1, 2**32, 2**64):
+            with pytest.raises(qp.QuantPipeError) as e:
+                call(cache, batch, *args, layer)
+            assert e.value.status == qp.QP_ERR_INVALID_ARG
+    for flags in (2, -1, 1 << 30):
+        d = qp.binding.KVAttentionDesc.from_buffer_copy(plan._desc)
+        d.flags = flags
+        assert qp.load().qp_kv_attention(ctx._h, C.byref(cache._desc), C.byref(batch._desc), C.byref(d), 0, q.data_ptr(), 0, 256, 64, q.data_ptr(),
+                                         256, 64, None, None) == qp.QP_ERR_INVALID_ARG
+    assert ctx.qp_get_status() == 0
 
 
 @pytest.mark.gpu
