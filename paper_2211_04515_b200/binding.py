@@ -746,16 +746,12 @@ class Context:
             raise QuantPipeError(QP_ERR_UNSUPPORTED_DTYPE, f"unsupported dtype {x.dtype}")
         return got
 
-    def _kv_here(self, *parts) -> None:
+    def _kv_here(self, *parts, layer: int = 0) -> None:
+        if not 0 <= layer < parts[0].layers:                        # (the call path would cut it to 32 bits)
+            raise QuantPipeError(QP_ERR_INVALID_ARG, f"layer {layer} of {parts[0].layers}")
         for p in parts:
             if p._index != self._index:
                 raise QuantPipeError(QP_ERR_INVALID_ARG, f"a cache, batch or plan on cuda:{p._index}, the context on {self.device}")
-
-    @staticmethod
-    def _kv_layer(cache: KVCache, layer: int) -> int:
-        if not 0 <= layer < cache.layers:
-            raise QuantPipeError(QP_ERR_INVALID_ARG, f"layer {layer} of {cache.layers}")
-        return layer
 
     def qp_kv_extend(self, cache: KVCache, batch: KVBatch) -> torch.Tensor:
         """Pages for the batch's new tokens; fills and returns batch.pos and adds to cache.lens."""
@@ -765,24 +761,24 @@ class Context:
 
     def qp_kv_append(self, cache: KVCache, batch: KVBatch, k: torch.Tensor, v: torch.Tensor, layer: int = 0) -> None:
         """Quantizes the step's keys and values [tokens, heads, head_dim] into the cache's pages."""
-        self._kv_here(cache, batch)
+        self._kv_here(cache, batch, layer=layer)
         code, kt, kh = self._kv_rows(k, batch.tokens, cache.heads, cache.head_dim, "k")
         v_code, vt, vh = self._kv_rows(v, batch.tokens, cache.heads, cache.head_dim, "v")
         if code != v_code:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "k and v of different types")
-        self._run("qp_kv_append", cache._at, batch._at, self._kv_layer(cache, layer), k, v, code, kt, kh, vt, vh)
+        self._run("qp_kv_append", cache._at, batch._at, layer, k, v, code, kt, kh, vt, vh)
 
     def qp_kv_gather(self, cache: KVCache, batch: KVBatch, k: torch.Tensor | None = None, v: torch.Tensor | None = None,
                      layer: int = 0, out_dtype: torch.dtype = torch.float32):
         """The batch's rows of the cache as the values they stand for: into k and v, or (both None) two new tensors of zeros."""
-        self._kv_here(cache, batch)
+        self._kv_here(cache, batch, layer=layer)
         if k is None and v is None:
             k, v = torch.zeros(2, batch.tokens, cache.heads, cache.head_dim, dtype=out_dtype, device=self.device)
         code, kt, kh = (None, 0, 0) if k is None else self._kv_rows(k, batch.tokens, cache.heads, cache.head_dim, "k")
         v_code, vt, vh = (code, 0, 0) if v is None else self._kv_rows(v, batch.tokens, cache.heads, cache.head_dim, "v")
         if code is not None and code != v_code:
             raise QuantPipeError(QP_ERR_INVALID_ARG, "k and v of different types")
-        self._run("qp_kv_gather", cache._at, batch._at, self._kv_layer(cache, layer), k, v, v_code, kt, kh, vt, vh)
+        self._run("qp_kv_gather", cache._at, batch._at, layer, k, v, v_code, kt, kh, vt, vh)
         return k, v
 
     def qp_kv_attention_plan(self, cache: KVCache, q_heads: int, window: int = 0, scale: float | None = None) -> KVAttention:
@@ -795,7 +791,7 @@ class Context:
                         out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
         """Attention of q [tokens, q_heads, head_dim] over the cache; writes out (q's type) and, if given, lse [tokens, q_heads].  Rows that no
         sequence of the batch has are left as they were in out, and zero in a new tensor (out None)."""
-        self._kv_here(cache, batch, plan)
+        self._kv_here(cache, batch, plan, layer=layer)
         code, qt, qh = self._kv_rows(q, batch.tokens, plan.q_heads, cache.head_dim, "q")
         at = plan._at
         if out is None:
@@ -809,7 +805,7 @@ class Context:
         if lse is not None and not (lse.dtype == torch.float32 and lse.get_device() == self._index and lse.is_contiguous()
                                     and lse.numel() >= batch.tokens * plan.q_heads):
             raise QuantPipeError(QP_ERR_INVALID_ARG, "lse must be a contiguous float32 tensor [tokens, q_heads]")
-        self._run("qp_kv_attention", cache._at, batch._at, at, self._kv_layer(cache, layer), q, code, qt, qh, out, ot, oh, lse)
+        self._run("qp_kv_attention", cache._at, batch._at, at, layer, q, code, qt, qh, out, ot, oh, lse)
         return out
 
     def qp_kv_fork(self, cache: KVCache, src: torch.Tensor, dst: torch.Tensor) -> None:
