@@ -592,7 +592,8 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
         const int all_hi = (int)min((int64_t)s.pos + row0 / a.group, (int64_t)0x7FFFFFFE) + 1;
         const int all_lo = a.window > 0 ? (int)min((int64_t)s.pos + last_row / a.group - a.window, (int64_t)0x7FFFFFFE) + 1 : 0;
         // p = 2^(s - m) in l; O holds sums of 2^(s + P_SHIFT - X) * v.  X follows the largest s + (power of two of the tile's V), of keys that the
-        // row sees: weights of 2^13 at most in fp16, and none lost that counts, whatever the other rows and tiles hold.
+        // row sees, as a whole number (so that it adds to V's powers and to m without rounding): weights of 2^13 at most in fp16, and none lost that
+        // counts, whatever the other rows and tiles hold.
         float m = M_NONE, X = M_NONE, l = 0.f;
         const int first_key = s.s0 * QP_KV_SLICE, u0 = s.u0, u1 = s.u1;
         for (int u = u0; u < u1; ++u, ++g) {
@@ -644,7 +645,7 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
                 }
                 most += ve;
                 if (__any_sync(0xFFFFFFFFu, top > m + M_SLACK || most > X + M_SLACK)) {     // rare: new references
-                    const float next = fmaxf(m, top), to = fmaxf(X, most), back = ex2(X - to);
+                    const float next = fmaxf(m, top), to = fmaxf(X, floorf(most)), back = ex2(X - to);
                     l *= ex2(m - next);
                     m = next;
                     X = to;

@@ -1,5 +1,5 @@
-"""The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, positions past the
-table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32, large batches,
+"""The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, large scores, positions
+past the table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32, large batches,
 launches that are refused, numbers past 32 bits."""
 import numpy as np
 import pytest
@@ -172,6 +172,29 @@ def test_values_of_many_sizes(ctx, case):
                 want, bound, _ = bound_of(q[b * new + i, g].double().cpu().numpy(), *rows, seen, dim ** -0.5, dtype, halves(dtype, dim, new * group))
                 off = np.abs(out[b * new + i, g] - want)
                 assert (off <= bound).all(), (b, i, g, float((off / bound).max()), float(off.max()), float(np.abs(want).max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dim,dtype,group,new", [(128, BF16, 4, 80), (64, BF16, 2, 100), (128, BF16, 4, 1), (128, F32, 2, 3)])
+def test_large_scores(ctx, dim, dtype, group, new, sign):
+    """Scores of 10^6 and more, whose own rounding moves the weights: where all rows of V are the same, so is the result."""
+    rng = np.random.default_rng(27)
+    n = 700
+    cache = make(rng, [n], 1, dim, 16)
+    base = rng.standard_normal(dim)
+    base *= dim ** 0.5 / np.linalg.norm(base)
+    k = (base * 600 + rng.standard_normal((n, 1, dim)) * 0.01).astype(np.float32) * sign
+    v = np.full((n, 1, dim), -2.0, np.float32)
+    ctx.qp_kv_append(cache, qp.KVBatch(ints([0]), start=ints([0, n]), tokens=n, max_new=n), *(torch.from_numpy(x.copy()).cuda() for x in (k, v)))
+    q = torch.from_numpy((base * rng.uniform(180, 420, (new, group, 1))).astype(np.float32)).cuda().to(dtype)
+    batch = qp.KVBatch(ints([n - new]), start=ints([0, new]), tokens=new, max_new=new)
+    out = ctx.qp_kv_attention(cache, batch, q, ctx.qp_kv_attention_plan(cache, group)).double().cpu().numpy()
+    assert ctx.qp_get_status() == 0
+    # The same weights in O and in l: what is left are the weights' rounding (2^-11; fp32 2^-21, and 2^-21 of exp2 where references move), sums
+    # of n / 8 steps and the result's own rounding.
+    share = (2.0 ** -11 if dtype == BF16 else 2.0 ** -19) + (n / 8 + 16) * 2.0 ** -24
+    assert (np.abs(out + 2) <= 2 * (share + torch.finfo(dtype).eps / 2 * (1 + share))).all(), float(np.abs(out + 2).max())
 
 
 @pytest.mark.gpu
