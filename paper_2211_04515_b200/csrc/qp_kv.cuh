@@ -67,19 +67,6 @@ __device__ __forceinline__ int qp_kv_start(const qp_kv_rows& r, int b)
 }
 __device__ __forceinline__ int qp_kv_slot(const qp_kv_rows& r, int b) { return r.slots ? qp_kv_ld(r.slots + b) : b; }
 
-// sequence that row `token` belongs to, -1 if none: the last b with start[b] <= token, if token < start[b + 1]
-__device__ __forceinline__ int qp_kv_find(const qp_kv_rows& r, int token)
-{
-    if (!r.start) return token < r.batch ? token : -1;
-    int lo = 0, hi = r.batch;                                    // start[lo] <= token (or lo = 0), start[hi] > token
-    if (qp_kv_start(r, 0) > token || qp_kv_start(r, r.batch) <= token) return -1;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (qp_kv_start(r, mid) <= token) lo = mid; else hi = mid;
-    }
-    return lo;
-}
-
 // page of token position p of a slot, -1 if the cache has none
 struct qp_kv_pages {
     const int32_t* table;

@@ -31,8 +31,9 @@
 //     sums start at zero and are added to the running ones by ordinary additions.
 //
 // Measured in a stream: 64 sequences of 200 to 8191 tokens, 32 query heads on 8 of 128: 59 us (212 MB, 3.6 TB/s over the whole call and 5.2
-// while codes are read; 49 % of the issue slots); 120001 and 131071 tokens, 64 query heads on 4: 57 us (143 MB, 2.5 TB/s: 16 queries to a
-// code); one sequence of 1021: 12 us; fp32, 24 sequences of 197 to 1500, 12 heads of 64: 18 us (15 MB).  A part of an item costs about 8 us beside
+// while codes are read; 50 % of the issue slots); 120001 and 131071 tokens, 64 query heads on 4: 59 us (143 MB, 2.4 TB/s: 16 queries to a
+// code; 44 % of the issue slots, 28 % of the matrix unit: latencies); one sequence of 1021: 11.6 us; fp32, 24 sequences of 197 to 1500, 12 heads
+// of 64: 18.7 us (15 MB).  A part of an item costs about 8 us beside
 // its codes, in latencies: its lengths and first codes 4, the reduction over warps 2, arrival and sum 2.
 #include "qp_kv.cuh"
 #include "qp_kv_attention.cuh"
@@ -59,8 +60,9 @@ constexpr int MIN_RUN = 2;
 // on it).
 constexpr unsigned REST_BLOCKS = 2;
 // Query rows of a sequence to a cached head from which on the tensor-memory kernel takes it.  This one against that, us, at 64 / 128 / 256
-// rows: 35 / 55 / 94 against 55 / 58 / 67 for 4 sequences of 4000 tokens and 8 heads; at 128 rows 94 against 71 for 16 of 4000
-// and 4 heads, 53 against 92 for one of 16000.
+// rows: 38 / 58 / 99 against 57 / 60 / 70 for 4 sequences of 4000 tokens and 8 heads.  Where the two meet also depends on how many items of
+// work there are, which a rule on rows does not know: at 128 rows 99 against 74 for 16 sequences of 4000 and 4 heads, 56 against 94 for one
+// of 16000 and 8 heads.  The rows are what a sequence knows about itself, whatever else is in its batch.
 constexpr int MANY = 160;
 
 template <int D, int NT, bool SPLIT> struct Cfg {

@@ -1,15 +1,15 @@
 // Attention over the 4-bit cache for many queries to a cached head (chunks of a prompt), bf16, on tcgen05.
 //
 // An item is 256 query rows of one cached head (row = token * group + query head of the group: all of them read the same
-// keys) as two tiles of 128, against the keys they see in tiles of 128.  Per key tile and query tile
-//     S = Q K^T    128 x 128 x D, both operands in shared memory, S in tensor memory
-//     P = 2^(S f - m)   a thread to a row
+// keys) as two tiles of 128, against the keys they see in tiles of 128, taken in halves of 64.  Per half and query tile
+//     S = Q K^T    128 x 64 x D, both operands in shared memory, S in tensor memory
+//     P = 2^(S f - X)   a thread to a row
 //     O += P V     P from tensor memory (over S), V in shared memory, O in tensor memory
 //
 // Roles: warps 0-3 and 4-7 are the rows of query tiles 0 and 1; warps 8-11 turn the cache's codes into fp16 operands; warp 12
 // issues the products.  The two query tiles take turns: one's softmax runs while the other's products do.
 //
-// What bounds it: 4 * 256 * 128 * D operations of the products (2048 cycles at D = 128 and the nominal rate) and as many cycles for
+// What it has to do: 4 * 256 * 128 * D operations of the products (2048 cycles at D = 128 and the nominal rate) and as many cycles for
 // the 32768 exponentials (16 a cycle).  So a softmax element gets three more operations and no more: the codes are not multiplied
 // as they are, as for few queries (their quantizers would cost two operations and shared-memory reads on every score and weight), but
 // as their values in fp16: a nibble under 1024's exponent is 1024 + code (or + 16 * code), less 1032 it is code - 8, and a fused
@@ -28,8 +28,9 @@
 //   - Registers: 128 a thread at launch; the softmax warps go to 160 (a row's 64 scores stay in registers), the issuing warp's group
 //     to 64 (2 * 160 + 128 + 64 = 4 * 128).  One copy of each hot loop: unrolled for each role they did not fit the instruction
 //     cache (1161 us against 936 for the case below).
-//   - Measured: 2048 tokens over 9001 and 16384, 32 query heads on 8 of 128: 838 us in short runs, 836 TFLOP/s, 935 with the GPU at its
-//     power limit.  52 % of the issue slots, tcgen05 44 % of the time.
+//   - Measured: 2048 tokens over 9001 and 16384, 32 query heads on 8 of 128: 952 us, 736 TFLOP/s, with the GPU at its power limit.
+//     52 % of the issue slots, tcgen05 43 % of the time: neither is full.  The scores' products take 6 KB of operands
+//     for 32 cycles at the nominal rate, more than the 128 bytes a cycle that shared memory gives; that this bounds them is not shown.
 //   - Every wait has a limit: a block that gives up raises QP_DEV_STREAM_TIMEOUT, its roles leave, the products in flight are
 //     waited for, tensor memory is freed.
 #include "qp_kv.cuh"
@@ -47,9 +48,9 @@ constexpr int MIN_RUN = 4;                       // key tiles that are worth a b
 constexpr int SEGS = 32;                         // parts of items that are listed at a time
 constexpr float M_NONE = -3.0e38f, M_SLACK = 8.f;
 constexpr int P_SHIFT = 5;                       // weights are 2^5 higher: up to 2^13 in fp16
-// A tile whose rows of V have largest values further apart than this (log2) has a power of two for each row.  Always so: 1330 us for 2048 tokens
-// over 9001 and 16384, never (no such tile): 956.  One power for rows 2^7 apart costs weights that stand at 2^8 or above seven of the 32 powers
-// of two that fp16 has below that.
+// A tile whose rows of V have largest values further apart than this (log2) has a power of two for each row.  2048 tokens over 9001 and 16384
+// take 1330 us if every tile does, 956 if none does.  (Rows 2^7 apart under one power lose 7 of the 39 powers of two that
+// fp16 has below 2^13.)
 constexpr int V_SPREAD = 7;
 
 template <int D> struct Cfg {

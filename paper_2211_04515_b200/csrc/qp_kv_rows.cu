@@ -414,7 +414,8 @@ int32_t launch_rows(qp_ctx* ctx, bool append, const qp_kv_cache_t* c, const qp_k
     a.k = k; a.v = v;
     a.kt = kt; a.kh = kh; a.vt = vt; a.vh = vh;
     a.status = ctx->d_status;
-    // Four rounds to a block at most (128 pairs of token and head), and enough blocks for two on every SM where there are the tokens
+    // Four rounds to a block at most (128 pairs of token and head; with more heads than that a token to a block, whose rounds are heads / 32), and
+    // enough blocks for two on every SM where there are the tokens
     int per_block = 4 * GROUPS / c->heads, fill = (b->tokens + 2 * ctx->sm_count - 1) / (2 * ctx->sm_count);
     if (per_block > fill) per_block = fill;
     per_block = per_block < 1 ? 1 : per_block > TOKENS ? TOKENS : per_block;
