@@ -644,12 +644,12 @@ int32_t qp_kv_gather(qp_ctx* ctx, const qp_kv_cache_t* h_cache, const qp_kv_batc
  *     out = sum_u p_u v_u,  p = softmax_u(scale * q . k_u)
  * with k_u and v_u the values that the cache's rows stand for.  q_heads is a multiple of the cache's heads; query head
  * g reads the cached head g / (q_heads / heads).  The step's own tokens are in the cache before (qp_kv_append).  Scores, softmax
- * and sums are fp32; out has q's type.  d_lse (or NULL): [tokens, q_heads] fp32, the natural logarithm of the sum
+ * and sums are fp32 (a score's parts, scale times the sum of q times codes and lo times the sum of q, have to stay within it); out has q's type.  d_lse (or NULL): [tokens, q_heads] fp32, the natural logarithm of the sum
  * of the exponentials.  A row that sees no key is 0 with lse -inf; a query with a non-finite element gives NaN in its row
  * only.  A token on a page that the table does not name, or behind its max_pages, counts as masked, with QP_DEV_KV_RANGE.
  * Where a bf16 sequence has 160 or more query rows to a cached head (its tokens times q_heads / heads) and head_dim is 64 or
- * 128, the values of K and V are rounded to fp16 (2^-11; K's no further than to 2^-34 of the largest among 128 keys) on the way into the products,
- * and so are the weights (2^-11, or 2^-22 of the largest weight times the largest value of its row of V); otherwise
+ * 128, the values of K and V are rounded to fp16 (2^-11, or 2^-22 of the row's largest) on the way into the products, and so are
+ * the weights (2^-11, or 2^-22 of the largest weight times the largest value of its row of V); otherwise
  * only the weights times V's scale are (fp32: they and q to 2^-22), or to 2^-32 of the query's largest of them: rows that a query does not
  * see, or gives next to no weight, have no part in that, however large they are.  A wait inside that kernel which does not end within the limit of
  * qp_set_wait_limit_for_testing raises QP_DEV_STREAM_TIMEOUT, as elsewhere.

@@ -18,8 +18,8 @@
 // The result, scale and the value of code 8 are each rounded to 11 bits, an eighth of what bf16 would lose.  (About code 0 instead: lo is
 // several times the middle of a row, and its rounding moves a whole row of scores; the result was 1.6 times as far off.)  fp16's range: each tile of K and of V is scaled by a power of two that takes its largest
 // value to [2^10, 2^11); queries are scaled by row.  K's power goes into the factor of the scores, V's into the exponent of
-// the weights (both are one number a tile).  A tile whose rows of V are of very different sizes has a power for each of them, which
-// goes into each weight's exponent.  Elements lie in the order 0 4 1 5 2 6 3 7 of each eight, in the operands and in O.
+// the weights (both are one number a tile).  A tile whose rows are of very different sizes has a power for each of them, which goes into
+// each score, or each weight's exponent.  Elements lie in the order 0 4 1 5 2 6 3 7 of each eight, in the operands and in O.
 //
 //   - Softmax reference raised only when a score passes it by 8 (log2).  O has another, of the scores plus V's powers: raised likewise, and then O
 //     is read from tensor memory, scaled and put back.
@@ -49,9 +49,11 @@ constexpr int SEGS = 32;                         // parts of items that are list
 constexpr float M_NONE = -3.0e38f, M_SLACK = 8.f;
 constexpr int P_SHIFT = 5;                       // weights are 2^5 higher: up to 2^13 in fp16
 // A tile whose rows of V have largest values further apart than this (log2) has a power of two for each row.  2048 tokens over 9001 and 16384
-// take 1330 us if every tile does, 956 if none does.  (Rows 2^7 apart under one power lose 7 of the 39 powers of two that
+// take 1743 us if every tile does, 956 if none does.  (Rows 2^7 apart under one power lose 7 of the 39 powers of two that
 // fp16 has below 2^13.)
 constexpr int V_SPREAD = 7;
+// The same for rows of K: a row's largest value stands at 2^-2 or above, so that what fp16 drops is 2^-23 of it.
+constexpr int K_SPREAD = 12;
 
 template <int D> struct Cfg {
     static constexpr int OPERAND = TILE * D * 2;                 // bytes of Q, K, V tiles
@@ -146,6 +148,21 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t* r)
                  : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld16(uint32_t at, float* x)
+{
+    uint32_t* r = reinterpret_cast<uint32_t*>(x);
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at));
+}
+__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t* r)
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]),
+                 "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+
 __device__ __forceinline__ float ex2(float x)
 {
     float r;
@@ -188,6 +205,9 @@ template <int ID> __device__ __forceinline__ void group_sync() { asm volatile("b
 __device__ __forceinline__ void group_sync(int id) { asm volatile("bar.sync %0, 128;" ::"r"(id) : "memory"); }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((unsigned)(e < -126 ? 1 : e > 127 ? 254 : e + 127) << 23); }
 
+// 2^e for e <= 0, to the smallest subnormal; 0 below
+__device__ __forceinline__ float pow2_down(int e) { return e >= -126 ? pow2(e) : e >= -149 ? __uint_as_float(1u << (149 + e)) : 0.f; }
+
 // ---------------------------------------------------------------------------- work
 
 // a part of an item: key tiles [u0, u1) of query rows tile * ROWS ..
@@ -206,10 +226,11 @@ struct Shared {
     int2 about[2];
     uint4 valid[2];
     float2 quant[2][2][TILE];                    // K's and V's quantizers of a tile
-    alignas(16) float row_power[2][TILE];        // where V's rows are scaled one by one (spread), a row's power of two less the tile's
+    // where rows are scaled one by one (spread: 1 V's, 2 K's): a row of V's power of two less the tile's; 2 to that for a row of K
+    alignas(16) float row_power[2][TILE], row_scale[2][TILE];
     int spread[2];
     unsigned amax[2][2][4];                      // per 32 keys the largest value of K and of V (bits of a float),
-    int vmin[2][4];                              // and the smallest power of a row of V
+    int amin[2][2][4];                           // and the smallest power of a row
     int last[2];
     Seg segs[SEGS];
 };
@@ -370,27 +391,38 @@ __device__ __forceinline__ void produce(const qp_kv_attn_args& a, Shared& sh, ch
             const int st = g & 1;
             const float4 quant = x.quant;
             // powers of two for the tile, which take its largest value to [2^10, 2^11) (not below -100: nothing to gain)
-            const unsigned mine = __float_as_uint(fmaxf(fabsf(quant.z), fabsf(fmaf(15.f, quant.w, quant.z))));
-            const unsigned ka = __reduce_max_sync(0xFFFFFFFFu, __float_as_uint(fmaxf(fabsf(quant.x), fabsf(fmaf(15.f, quant.y, quant.x)))));
-            const unsigned va = __reduce_max_sync(0xFFFFFFFFu, mine);
-            const int own = max((int)(mine >> 23) - 137, -100), vmin = __reduce_min_sync(0xFFFFFFFFu, x.there >> lane & 1u ? own : 1000);
-            if (lane == 0) { sh.amax[st][0][p >> 5] = ka; sh.amax[st][1][p >> 5] = va; sh.vmin[st][p >> 5] = vmin; }
+            const unsigned k_bits = __float_as_uint(fmaxf(fabsf(quant.x), fabsf(fmaf(15.f, quant.y, quant.x))));
+            const unsigned v_bits = __float_as_uint(fmaxf(fabsf(quant.z), fabsf(fmaf(15.f, quant.w, quant.z))));
+            const int k_own = max((int)(k_bits >> 23) - 137, -100), v_own = max((int)(v_bits >> 23) - 137, -100);
+            const unsigned ka = __reduce_max_sync(0xFFFFFFFFu, k_bits), va = __reduce_max_sync(0xFFFFFFFFu, v_bits);
+            // (a row of zeros is one however it is scaled; of V it may have all the weight, and then the others must not lose theirs)
+            const int kmin = __reduce_min_sync(0xFFFFFFFFu, k_bits ? k_own : 1000);
+            const int vmin = __reduce_min_sync(0xFFFFFFFFu, x.there >> lane & 1u ? v_own : 1000);
+            if (lane == 0) {
+                sh.amax[st][0][p >> 5] = ka; sh.amax[st][1][p >> 5] = va;
+                sh.amin[st][0][p >> 5] = kmin; sh.amin[st][1][p >> 5] = vmin;
+            }
             sh.quant[st][0][p] = make_float2(quant.x, quant.y);
             sh.quant[st][1][p] = make_float2(quant.z, quant.w);
             group_sync<1>();
             unsigned kb = 0, vb = 0;
-            int least = 1000;
+            int k_least = 1000, v_least = 1000;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) { kb = max(kb, sh.amax[st][0][w]); vb = max(vb, sh.amax[st][1][w]); least = min(least, sh.vmin[st][w]); }
+            for (int w = 0; w < 4; ++w) {
+                kb = max(kb, sh.amax[st][0][w]); vb = max(vb, sh.amax[st][1][w]);
+                k_least = min(k_least, sh.amin[st][0][w]); v_least = min(v_least, sh.amin[st][1][w]);
+            }
             const int ke = max((int)(kb >> 23) - 137, -100), ve = max((int)(vb >> 23) - 137, -100);
-            const bool spread = ve - least > V_SPREAD;           // (the same in all threads)
-            const float kf = pow2(-ke), vf = spread ? 1.f : pow2(-ve);
+            const int spread = (ve - v_least > V_SPREAD ? 1 : 0) | (ke - k_least > K_SPREAD ? 2 : 0);      // (the same in all threads)
+            const float kf = spread & 2 ? 1.f : pow2(-ke), vf = spread & 1 ? 1.f : pow2(-ve);
             if (g >= 2) wait(sh, &sh.kv_empty[st], ((g >> 1) + 1) & 1, a.wait_cycles);
             __syncwarp();
             if (spread) {
-                const float f = pow2(-own);
-                sh.quant[st][1][p] = make_float2(quant.z * f, quant.w * f);
-                sh.row_power[st][p] = (float)(own - ve);
+                const float k_f = pow2(-k_own), v_f = pow2(-v_own);
+                if (spread & 2) sh.quant[st][0][p] = make_float2(quant.x * k_f, quant.y * k_f);
+                if (spread & 1) sh.quant[st][1][p] = make_float2(quant.z * v_f, quant.w * v_f);
+                sh.row_scale[st][p] = spread & 2 ? pow2_down(k_own - ke) : 1.f;
+                sh.row_power[st][p] = spread & 1 ? (float)(v_own - ve) : 0.f;
                 group_sync<1>();
             }
             char* to = stages + st * (2 * C::OPERAND);
@@ -613,97 +645,125 @@ __device__ __forceinline__ void softmax(const qp_kv_attn_args& a, Shared& sh, ch
                 wait(sh, &sh.s_full[t][h], g & 1, a.wait_cycles);
                 __syncwarp();
                 fence_after();
-                float x[HALF];
-                tmem_ld32(s_at + h * HALF, x);
-                tmem_ld32(s_at + h * HALF + 32, x + 32);
-                wait_ld(x);
-                if (!whole) {
+                // which of 32 keys the row sees
+                auto seen_of = [&](int c) {
+                    if (whole) return 0xFFFFFFFFu;
+                    const int up = hi - t0 - 32 * c, down = a.window > 0 ? hi - a.window - t0 - 32 * c : -1;   // keys (down, up]
+                    unsigned seen = h ? (c ? v4.w : v4.z) : (c ? v4.y : v4.x);
+                    seen &= up < 0 ? 0u : up >= 31 ? 0xFFFFFFFFu : (2u << up) - 1u;
+                    return seen & (down < 0 ? 0xFFFFFFFFu : down >= 31 ? 0u : ~((2u << down) - 1u));
+                };
+                // rows scaled one by one (uncommon): 16 keys at a time, read again for the weights, so that this code is short
+                const float *scale = sh.row_scale[st] + h * HALF, *power = sh.row_power[st] + h * HALF;
+                auto piece = [&](int c, float (&y)[16], float (&pw)[16]) {
+                    tmem_ld16(s_at + h * HALF + 16 * c, y);
+                    const unsigned seen = seen_of(c >> 1) >> (16 * (c & 1));
+                    float sc[16];
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4) {
+                        const float4 r = *reinterpret_cast<const float4*>(scale + 16 * c + e), w = *reinterpret_cast<const float4*>(power + 16 * c + e);
+                        sc[e] = r.x; sc[e + 1] = r.y; sc[e + 2] = r.z; sc[e + 3] = r.w;
+                        pw[e] = w.x; pw[e + 1] = w.y; pw[e + 2] = w.z; pw[e + 3] = w.w;
+                    }
+                    wait_ld(y);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) y[e] = seen >> e & 1u ? y[e] * sc[e] : -inf;
+                };
+                // new references where a score, or a score plus V's power, has passed them by too much (rare)
+                auto refer = [&](float top, float most) {
+                    if (__any_sync(0xFFFFFFFFu, top > m + M_SLACK || most > X + M_SLACK)) {     // rare: new references
+                        const float next = fmaxf(m, top), to = fmaxf(X, floorf(most)), back = ex2(X - to);
+                        l *= ex2(m - next);
+                        m = next;
+                        X = to;
+                        if (u > u0 || h > 0) {
+                            wait(sh, &sh.pv_done[t][h ^ 1], (h ? g : g - 1) & 1, a.wait_cycles);      // of the half before
+                            __syncwarp();
+                            fence_after();
+#pragma unroll 1
+                            for (int c = 0; c < D / 32; ++c) {
+                                float y[32];
+                                tmem_ld32(o_at + 32 * c, y);
+                                wait_ld(y);
+#pragma unroll
+                                for (int e = 0; e < 32; ++e) y[e] *= back;
+                                tmem_st32(o_at + 32 * c, y);
+                            }
+                            wait_st();
+                        }
+                    }
+                };
+                if (!spread) {
+                    float x[HALF];
+                    tmem_ld32(s_at + h * HALF, x);
+                    tmem_ld32(s_at + h * HALF + 32, x + 32);
+                    wait_ld(x);
+                    if (!whole) {
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const unsigned seen = seen_of(c);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) x[32 * c + e] = seen >> e & 1u ? x[32 * c + e] : -inf;
+                        }
+                    }
+                    float top4[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                    for (int c = 4; c < HALF; c += 8)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) top4[e] = c + 4 + e < HALF ? qp_max3(top4[e], x[c + e], x[c + 4 + e]) : fmaxf(top4[e], x[c + e]);
+                    const float top = fmaxf(qp_max3(top4[0], top4[1], top4[2]), top4[3]) * f;
+                    refer(top, top + ve);
+                    // (where V is so small against what O holds that its weights leave fp16, they must not leave fp32, for the sum's sake)
+                    const float sub = fmaxf((float)P_SHIFT + ve - X, (float)(P_SHIFT - 90) - m);
+                    const qp_f2 f2 = qp_pack2(f, f), sub2 = qp_pack2(sub, sub);
+                    qp_f2 sum = qp_pack2(0.f, 0.f), sum1 = sum;
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
-                        const int up = hi - t0 - 32 * c, down = a.window > 0 ? hi - a.window - t0 - 32 * c : -1;   // keys (down, up]
-                        unsigned seen = h ? (c ? v4.w : v4.z) : (c ? v4.y : v4.x);
-                        seen &= up < 0 ? 0u : up >= 31 ? 0xFFFFFFFFu : (2u << up) - 1u;
-                        seen &= down < 0 ? 0xFFFFFFFFu : down >= 31 ? 0u : ~((2u << down) - 1u);
+                        uint32_t w[16];
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) x[32 * c + e] = seen >> e & 1u ? x[32 * c + e] : -inf;
-                    }
-                }
-                float top4[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-                for (int c = 4; c < HALF; c += 8)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) top4[e] = c + 4 + e < HALF ? qp_max3(top4[e], x[c + e], x[c + 4 + e]) : fmaxf(top4[e], x[c + e]);
-                const float top = fmaxf(qp_max3(top4[0], top4[1], top4[2]), top4[3]) * f;
-                const float* power = sh.row_power[st] + h * HALF;
-                float most = top;
-                if (spread) {                                    // uncommon: rows of V scaled one by one
-                    most = -inf;
-#pragma unroll
-                    for (int c = 0; c < HALF; c += 4) {
-                        const float4 r = *reinterpret_cast<const float4*>(power + c);
-                        most = fmaxf(qp_max3(most, fmaf(x[c], f, r.x), fmaf(x[c + 1], f, r.y)), fmaxf(fmaf(x[c + 2], f, r.z), fmaf(x[c + 3], f, r.w)));
-                    }
-                }
-                most += ve;
-                if (__any_sync(0xFFFFFFFFu, top > m + M_SLACK || most > X + M_SLACK)) {     // rare: new references
-                    const float next = fmaxf(m, top), to = fmaxf(X, floorf(most)), back = ex2(X - to);
-                    l *= ex2(m - next);
-                    m = next;
-                    X = to;
-                    if (u > u0 || h > 0) {
-                        wait(sh, &sh.pv_done[t][h ^ 1], (h ? g : g - 1) & 1, a.wait_cycles);      // of the half before
-                        __syncwarp();
-                        fence_after();
-#pragma unroll 1
-                        for (int c = 0; c < D / 32; ++c) {
-                            float y[32];
-                            tmem_ld32(o_at + 32 * c, y);
-                            wait_ld(y);
-#pragma unroll
-                            for (int e = 0; e < 32; ++e) y[e] *= back;
-                            tmem_st32(o_at + 32 * c, y);
+                        for (int e = 0; e < 16; ++e) {
+                            float y0, y1;
+                            qp_unpack2(qp_fma2(qp_pack2(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), f2, sub2), y0, y1);
+                            y0 = ex2(y0);
+                            y1 = ex2(y1);
+                            if (e & 1) sum1 = qp_add2(sum1, qp_pack2(y0, y1));
+                            else sum = qp_add2(sum, qp_pack2(y0, y1));
+                            w[e] = half2_of(y0, y1);
                         }
-                        wait_st();
+                        tmem_st16(s_at + h * HALF + 16 * c, w);
                     }
-                }
-                float sub = (float)P_SHIFT + ve - X, fw = f, lift = 0.f;
-                if (!spread) {
-                    // (where V is so small against what O holds that its weights leave fp16, they must not leave fp32, for the sum's sake)
-                    sub = fmaxf(sub, (float)(P_SHIFT - 90) - m);
-                    lift = ex2(-m - sub);
+                    float s0, s1;
+                    qp_unpack2(qp_add2(sum, sum1), s0, s1);
+                    l = fmaf(s0 + s1, ex2(-m - sub), l);
                 } else {
-                    float s0 = 0.f, s1 = 0.f;
+                    float top = -inf, most = -inf;
+#pragma unroll 1
+                    for (int c = 0; c < HALF / 16; ++c) {
+                        float y[16], pw[16];
+                        piece(c, y, pw);
 #pragma unroll
-                    for (int c = 0; c < HALF; c += 4) {
-                        const float4 r = *reinterpret_cast<const float4*>(power + c);
-                        s0 += ex2(fmaf(x[c], f, -m)) + ex2(fmaf(x[c + 1], f, -m));
-                        s1 += ex2(fmaf(x[c + 2], f, -m)) + ex2(fmaf(x[c + 3], f, -m));
-                        x[c] = fmaf(x[c], f, r.x); x[c + 1] = fmaf(x[c + 1], f, r.y);
-                        x[c + 2] = fmaf(x[c + 2], f, r.z); x[c + 3] = fmaf(x[c + 3], f, r.w);
+                        for (int e = 0; e < 16; e += 2) {
+                            top = qp_max3(top, y[e], y[e + 1]);
+                            most = qp_max3(most, fmaf(y[e], f, pw[e]), fmaf(y[e + 1], f, pw[e + 1]));
+                        }
                     }
-                    l += s0 + s1;
-                    fw = 1.f;
-                }
-                const qp_f2 f2 = qp_pack2(fw, fw), sub2 = qp_pack2(sub, sub);
-                qp_f2 sum = qp_pack2(0.f, 0.f), sum1 = sum;
+                    refer(top * f, most + ve);
+                    const float sub = (float)P_SHIFT + ve - X;
+                    float sum = 0.f;
+#pragma unroll 1
+                    for (int c = 0; c < HALF / 16; ++c) {        // (a piece's weights lie over scores that were read before)
+                        float y[16], pw[16];
+                        uint32_t w[8];
+                        piece(c, y, pw);
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        float y0, y1;
-                        qp_unpack2(qp_fma2(qp_pack2(x[32 * c + 2 * e], x[32 * c + 2 * e + 1]), f2, sub2), y0, y1);
-                        y0 = ex2(y0);
-                        y1 = ex2(y1);
-                        if (e & 1) sum1 = qp_add2(sum1, qp_pack2(y0, y1));
-                        else sum = qp_add2(sum, qp_pack2(y0, y1));
-                        w[e] = half2_of(y0, y1);
+                        for (int e = 0; e < 16; e += 2) {
+                            sum += ex2(fmaf(y[e], f, -m)) + ex2(fmaf(y[e + 1], f, -m));
+                            w[e / 2] = half2_of(ex2(fmaf(y[e], f, pw[e]) + sub), ex2(fmaf(y[e + 1], f, pw[e + 1]) + sub));
+                        }
+                        tmem_st8(s_at + h * HALF + 8 * c, w);
                     }
-                    tmem_st16(s_at + h * HALF + 16 * c, w);
+                    l += sum;
                 }
-                float s0, s1;
-                qp_unpack2(qp_add2(sum, sum1), s0, s1);
-                l = fmaf(s0 + s1, lift, l);
                 wait_st();
                 fence_before();
                 arrive(&sh.p_full[t][h]);

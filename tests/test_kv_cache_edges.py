@@ -1,4 +1,4 @@
-"""The 4-bit cache of keys and values where it can go wrong: rows of V that a query does not see or gives no weight, large scores, positions
+"""The 4-bit cache of keys and values where it can go wrong: rows that a query does not see or gives no weight, large scores, positions
 past the table, more sequences than rows, rows that no sequence writes, queries that see nothing or whose sum passes fp32, large batches,
 launches that are refused, numbers past 32 bits."""
 import numpy as np
@@ -29,11 +29,11 @@ def bound_of(q, k, v, seen, scale, dtype, in_halves):
     weights = eps * (p * vs) @ vc / l + n * 15 * 2.0 ** -32 * (p * vs).max() / l
     v_off = 0.0
     if in_halves:
-        # K and V in fp16: of the value 2^-11, of the middle of the row 2^-11, of the scale 2^-11 times at most 8; K by a tile's power of
-        # two (2^-34 of the tile's largest, here of the largest seen)
+        # K and V in fp16: of the value 2^-11, of the middle of the row 2^-11, of the scale 2^-11 times at most 8.  A row of K has its
+        # largest value at 2^-2 or above, so a subnormal's 2^-25, twice, is 2^-22 of that.
         def rounding(x, lo, scale):
             return 2.0 ** -11 * (np.abs(x) + (np.abs(lo + 8 * scale) + 8 * scale)[:, None])
-        ds = ds + abs(scale) * ((rounding(kv, klo, ks) + 2.0 ** -34 * np.abs(kv).max()) @ np.abs(q))
+        ds = ds + abs(scale) * ((rounding(kv, klo, ks) + (2.0 ** -22 * np.abs(kv).max(1))[:, None]) @ np.abs(q))
         # Weights: 2^-11, and 2^-25 below the normal numbers.  A row's own largest value stands at 2^3 or above in its tile (below 2^11), so
         # that a subnormal value's 2^-25, twice, is at most 2^-26 of it.  The weight that O's reference was taken from is 2^5 or more, so
         # the largest p * (row's largest value) stands at 2^8 or above, and 2^-25 * 2^11 is 2^-22 of that.
@@ -125,6 +125,49 @@ def test_values_without_weight(ctx, case, octaves):
     for times in (1.0, 2.0 ** octaves):
         v[big + later + before] *= times
         ctx.qp_kv_append(cache, qp.KVBatch(ints([0]), start=ints([0, n]), tokens=n, max_new=n), k, torch.from_numpy(v.astype(np.float32)).cuda())
+        got.append(ctx.qp_kv_attention(cache, batch, q, plan, out=torch.empty_like(q)).double().cpu().numpy())
+        rows.append(ref.sequence(cache.pool[0].cpu().numpy(), cache.table[0].cpu().numpy(), 0, n, page, dim))
+    assert ctx.qp_get_status() == 0
+    qn = q.double().cpu().numpy()
+    u = np.arange(n)
+    for i in range(new):
+        t = n - new + i
+        seen = (u <= t) & ((u > t - window) if window else True)
+        for g in range(group):
+            wants = [bound_of(qn[i, g], *r, seen, dim ** -0.5, dtype, halves(dtype, dim, new * group)) for r in rows]
+            apart = np.abs(got[1][i, g] - got[0][i, g])
+            limit = np.abs(wants[1][0] - wants[0][0]) + np.maximum(wants[0][2], wants[1][2])
+            assert (apart <= limit).all(), (i, g, float((apart / limit).max()), float(apart.max()), float(np.abs(wants[0][0]).max()))
+            for have, (want, bound, _) in zip(got, wants):
+                off = np.abs(have[i, g] - want)
+                assert (off <= bound).all(), (i, g, float((off / bound).max()), float(off.max()), float(np.abs(want).max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("octaves", [12, 24, 60, 100])
+@pytest.mark.parametrize("case", OUTLIERS, ids=str)
+def test_keys_without_weight(ctx, case, octaves):
+    """The same with rows of K: 2^octaves times as large as the others, masked, in front of the window or far below the other scores."""
+    dim, dtype, group, new, window = case
+    rng = np.random.default_rng(dim + new + octaves + 1)
+    n, page = 1999, 32
+    cache = make(rng, [n], 1, dim, page)
+    base = rng.standard_normal(dim)
+    base *= dim ** 0.5 / np.linalg.norm(base)
+    k = rng.standard_normal((n, 1, dim)) * 0.7
+    v = torch.from_numpy((rng.standard_normal((n, 1, dim)) * rng.uniform(0.3, 1.5, (n, 1, 1))).astype(np.float32)).cuda()
+    large = [5, 700, n - new - 1, n - 1] + ([n - new // 2] if new > 2 else [])
+    large += [n - new - window - 1, n - new - window - 5] if window else []
+    k[large] = -8 * base                                            # 8 * sqrt(dim) below, in nats
+    k[40] = 0
+    k[41] *= 2.0 ** -30
+    q = torch.from_numpy((base + 1.2 * rng.standard_normal((new, group, dim))).astype(np.float32)).cuda().to(dtype)
+    batch = qp.KVBatch(ints([n - new]), start=ints([0, new]), tokens=new, max_new=new)
+    plan = ctx.qp_kv_attention_plan(cache, group, window)
+    got, rows = [], []
+    for times in (1.0, 2.0 ** octaves):
+        k[large] *= times
+        ctx.qp_kv_append(cache, qp.KVBatch(ints([0]), start=ints([0, n]), tokens=n, max_new=n), torch.from_numpy(k.astype(np.float32)).cuda(), v)
         got.append(ctx.qp_kv_attention(cache, batch, q, plan, out=torch.empty_like(q)).double().cpu().numpy())
         rows.append(ref.sequence(cache.pool[0].cpu().numpy(), cache.table[0].cpu().numpy(), 0, n, page, dim))
     assert ctx.qp_get_status() == 0
